@@ -225,6 +225,77 @@ LIME_API lime_status lime_score_candidates_head(lime_ctx* ctx, const void* link_
                                        const int32_t* cand_ids, int64_t corpus_rows, int32_t* dev_flag, float* logits,
                                        void* ws, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------------------
+ * The user encoder that LIME is measured against (the paper's softmax "skyline"): every event of a history attends to the events
+ * before it, candidates or drafted continuations attend to the history and to themselves, and the history's keys and values stay in
+ * a cache between requests.  Three calls, for inference: norms and rotation on the way into the cache, attention over whole histories,
+ * attention of a few new rows over the cache.
+ *
+ * Rows are packed user after user: row t of a tensor of h heads is h * d_h contiguous elements of config.dtype (head after head) at
+ * t * stride; strides are in elements, at least h * d_h and a multiple of 16 bytes, so queries, keys and values may be parts of one
+ * wider row.  Offsets are device int32 [B+1], non-decreasing, off[0] = 0 (as lime_lengths_to_offsets leaves them); rows from off[B] on
+ * belong to nobody: of the outputs they are left as they were.  Offsets past the number of rows given are cut to it.  Outputs must not
+ * overlap inputs unless a comment allows it.  The calls run on the device the context was created on, which must be current. */
+typedef struct lime_sequence {
+  int32_t Hq, Hkv, d_h;       /* query heads, heads of keys and values (Hq % Hkv == 0, Hq / Hkv <= 64; query head h reads
+                                 key head h / (Hq / Hkv)), features of a head: a multiple of 8, 8..128; Hq <= 1024          */
+  float attn_scale;           /* softmax scale; 0 means 1/sqrt(d_h)                                                         */
+  float norm_eps;             /* of the norms; 0 means 1e-6                                                                 */
+  int32_t rot_dim;            /* leading features of a head that are rotated by position: even, 0..d_h                      */
+  int32_t rot_interleaved;    /* 0: features i and i + rot_dim / 2 form a pair; 1: features 2i and 2i + 1                   */
+  double rot_base;            /* pair i turns by position * rot_base^(-2i / rot_dim) radians; 0 means 10000; 1 .. 1e30      */
+} lime_sequence;
+
+/* Set-up: keeps a copy of the shape (host only, nothing is launched).  The calls below return LIME_NOT_READY before it. */
+LIME_API lime_status lime_set_sequence(lime_ctx* ctx, const lime_sequence* seq);
+
+/* Norm of each head and rotation by position, in one pass:
+ *   y = x * rsqrt(mean(x^2) + norm_eps) * gamma,  then each pair (a, b) of y to (a cos - b sin, b cos + a sin)
+ * for q [rows x Hq x d_h] and k [rows x Hkv x d_h]; statistics, angles and products in 32 bits or more, one rounding at the end.  The
+ * angle is formed from the whole position in fixed point, so positions far out lose nothing; negative ones turn backwards.
+ * gamma_q / gamma_k [d_h] in config.dtype, NULL = ones.  positions [rows] device int32 (may be NULL with rot_dim = 0).
+ * q_out, k_out [rows x ..] with strides of their own; each may be its input itself (same pointer and stride).
+ * Cache: with cache_k [cache_rows x Hkv x d_h] (contiguous rows, e.g. pages one after the other), row t of the new keys goes to row
+ * slots[t] of it as well, and row t of v [rows x Hkv x d_h] as it is to row slots[t] of cache_v; k_out may then be NULL.  A slot of -1
+ * writes nothing (padding); another slot outside [0, cache_rows) writes nothing and lowers *dev_flag (device int32, nullable, caller
+ * initialises it to INT32_MAX) to the smallest such t.  Two rows with the same slot: which of them stays is not determined.
+ * v and cache_v are given together, and only with cache_k; slots and cache_k are given together. */
+LIME_API lime_status lime_norm_rotate(lime_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                             int64_t v_stride, const void* gamma_q, const void* gamma_k, const int32_t* positions, int64_t rows,
+                             void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* cache_k, void* cache_v,
+                             int64_t cache_rows, const int32_t* slots, int32_t* dev_flag, void* stream);
+
+/* Scratch for the two attention calls: enough for up to B users with `rows` query rows in all, whatever the lengths of their keys.
+ * 0 on invalid arguments or before lime_set_sequence. */
+LIME_API size_t lime_sequence_workspace_bytes(const lime_ctx* ctx, int32_t B, int64_t rows);
+
+/* Causal attention over packed histories:
+ *   out[i, h, :] = sum_j softmax_j(attn_scale <q[i, h, :], k[j, h', :]>) v[j, h', :]   over the keys j <= i + n_keys - n_queries
+ * of i's user (i, j counted within the user): the last query sees every key, so new rows behind older ones are queries fewer than
+ * keys.  q [q_rows x Hq x d_h] by off, k and v [kv_rows x Hkv x d_h] by kv_off (NULL: the same rows as the queries', kv_rows =
+ * q_rows); out [q_rows x Hq x d_h].  A query that sees no key (more queries than keys, an empty history) gets zeros.  What a query does
+ * not see has no influence on it, infinities and NaN included.  bf16: products of bf16 values in fp32, probabilities rounded to bf16 for
+ * the value product (their sum is not), one rounding of the result; fp32: all in fp32. */
+LIME_API lime_status lime_attend_history(lime_ctx* ctx, const void* q, int64_t q_stride, const int32_t* off, const void* k,
+                                int64_t k_stride, const void* v, int64_t v_stride, const int32_t* kv_off, int32_t B, int64_t q_rows,
+                                int64_t kv_rows, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
+
+/* Attention of new rows over a cache in pages, and over one another along a tree.  User b's cached keys are its first ctx_len[b] rows:
+ * row j lies in page page_table[b, j / page_rows] (device int32 [B x max_pages]) at j % page_rows of cache_k, cache_v [n_pages x
+ * page_rows x Hkv x d_h]; page_rows is a power of two, 16..4096.  ctx_len is device int32 [B], cut to 0 .. max_pages * page_rows.  A
+ * page outside [0, n_pages) among those reads as rows of zeros and lowers *dev_flag (nullable, as above) to the smallest such position
+ * b * max_pages + i.  Pages may be shared by users.
+ * q [rows x Hq x d_h] and out by off.  Every row sees the user's cached rows, and:
+ *   tree_k = tree_v = NULL: nothing else (the rows' own keys are in the cache already: one new event, or several that all see it all);
+ *   tree_k, tree_v [rows x Hkv x d_h]: the row itself and its ancestors.  parent [rows] device int32: the row's parent as an index among
+ *   the user's rows, smaller than its own, anything else makes it a root; parent = NULL: all are roots (a list of candidates).
+ * A row that sees nothing gets zeros.  Rounding, infinities and NaN as in lime_attend_history. */
+LIME_API lime_status lime_attend_tree(lime_ctx* ctx, const void* q, int64_t q_stride, const int32_t* off, const int32_t* parent,
+                             const void* tree_k, int64_t tree_k_stride, const void* tree_v, int64_t tree_v_stride, int32_t B,
+                             int64_t rows, const void* cache_k, const void* cache_v, int64_t n_pages, int32_t page_rows,
+                             const int32_t* page_table, int32_t max_pages, const int32_t* ctx_len, int32_t* dev_flag, void* out,
+                             int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
+
 /* Allocation-free precompute (the paper has no counterpart: this exists for hosts that must not allocate).
  * Same result as lime_create + lime_set_weights + lime_precompute_candidate_links, for callers that cannot call
  * cudaMalloc at this point - a serving process whose device memory pool is frozen after start-up, or code running

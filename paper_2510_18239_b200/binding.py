@@ -56,11 +56,17 @@ class lime_ffn(ctypes.Structure):
                 ("W", ctypes.c_void_p * (LIME_FFN_MAX_HIDDEN + 1)), ("b", ctypes.c_void_p * (LIME_FFN_MAX_HIDDEN + 1))]
 
 
+class lime_sequence(ctypes.Structure):
+    _fields_ = [("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d_h", ctypes.c_int32), ("attn_scale", ctypes.c_float),
+                ("norm_eps", ctypes.c_float), ("rot_dim", ctypes.c_int32), ("rot_interleaved", ctypes.c_int32), ("rot_base", ctypes.c_double)]
+
+
 EXPORTS = ("lime_create", "lime_destroy", "lime_set_weights", "lime_workspace_bytes", "lime_lengths_to_offsets",
            "lime_gather_history", "lime_gather_history_normalized", "lime_precompute_candidate_links", "lime_xor_layer",
            "lime_encode_user", "lime_encode_user_normalized",
            "lime_score_candidates", "lime_pack_corpus_cache", "lime_score_candidates_packed", "lime_set_context_mlp", "lime_contextualize_links", "lime_set_head",
-           "lime_head_workspace_bytes", "lime_score_candidates_head", "lime_precompute_candidate_links_noalloc", "lime_device_status", "lime_selftest_wait_expiry", "lime_profile_start", "lime_profile_stop", "lime_last_cuda_error",
+           "lime_head_workspace_bytes", "lime_score_candidates_head", "lime_set_sequence", "lime_norm_rotate", "lime_sequence_workspace_bytes",
+           "lime_attend_history", "lime_attend_tree", "lime_precompute_candidate_links_noalloc", "lime_device_status", "lime_selftest_wait_expiry", "lime_profile_start", "lime_profile_stop", "lime_last_cuda_error",
            "lime_version")
 
 _lib_handle = None
@@ -99,6 +105,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.lime_head_workspace_bytes.restype = sz
     lib.lime_score_candidates_head.argtypes = [vp, vp, i32, vp, vp, vp, i32, i64, vp, i64, vp, vp, vp, sz, vp]
     lib.lime_precompute_candidate_links_noalloc.argtypes = [i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, i64, vp, vp]
+    lib.lime_set_sequence.argtypes = [vp, ctypes.POINTER(lime_sequence)]
+    lib.lime_norm_rotate.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp]
+    lib.lime_sequence_workspace_bytes.argtypes = [vp, i32, i64]
+    lib.lime_sequence_workspace_bytes.restype = sz
+    lib.lime_attend_history.argtypes = [vp, vp, i64, vp, vp, i64, vp, i64, vp, i32, i64, i64, vp, i64, vp, sz, vp]
+    lib.lime_attend_tree.argtypes = [vp, vp, i64, vp, vp, vp, i64, vp, i64, i32, i64, vp, vp, i64, i32, vp, i32, vp, vp, vp, i64, vp, sz, vp]
     lib.lime_device_status.argtypes = [vp, ctypes.POINTER(i32)]
     lib.lime_selftest_wait_expiry.argtypes = [vp, i32, vp]
     lib.lime_profile_start.argtypes = [i32]
@@ -108,7 +120,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         if name in ("lime_last_cuda_error", "lime_version"):
             fn.restype = ctypes.c_char_p
             fn.argtypes = []
-        elif name not in ("lime_workspace_bytes", "lime_head_workspace_bytes"):
+        elif name not in ("lime_workspace_bytes", "lime_head_workspace_bytes", "lime_sequence_workspace_bytes"):
             fn.restype = ctypes.c_int
     if path is None:
         _lib_handle = lib
@@ -304,6 +316,117 @@ def lime_score_candidates_head(ctx: int, link_states: torch.Tensor, B: int, cand
            "lime_score_candidates_head")
 
 
+# ---- the sequence path: rows of heads, [rows x heads x d_h], each row contiguous, rows at any stride
+def _rows(t: Optional[torch.Tensor], heads: int, d_h: int, dtype: torch.dtype, device: torch.device, name: str, rows: Optional[int] = None):
+    """(pointer, row stride) of `t`, or (None, 0) of None.  ValueError for what the library would read wrongly."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"expected a torch.Tensor, got {type(t).__name__}")
+    if not t.is_cuda or t.device != device or t.dtype != dtype or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d_h:
+        raise ValueError(f"{name}: expected {dtype} rows [n x {heads} x {d_h}] on {device}")
+    if rows is not None and t.shape[0] != rows:
+        raise ValueError(f"{name}: expected {rows} rows, got {t.shape[0]}")
+    if (d_h > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d_h):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * d_h
+
+
+def _ints(t: Optional[torch.Tensor], device: torch.device, name: str, n: Optional[int] = None) -> Optional[int]:
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"expected a torch.Tensor, got {type(t).__name__}")
+    if not t.is_cuda or t.device != device or t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise ValueError(f"{name}: expected contiguous int32 on {device}" + ("" if n is None else f", {n} of them"))
+    return t.data_ptr()
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, device: torch.device, name: str) -> Optional[int]:
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"expected a torch.Tensor, got {type(t).__name__}")
+    if not t.is_cuda or t.device != device or t.dtype != dtype or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{name}: expected {n} contiguous values of {dtype} on {device}")
+    return t.data_ptr()
+
+
+def _pages(t: torch.Tensor, heads: int, d_h: int, dtype: torch.dtype, device: torch.device, name: str) -> Optional[int]:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"expected a torch.Tensor, got {type(t).__name__}")
+    if (not t.is_cuda or t.device != device or t.dtype != dtype or t.dim() != 4 or t.shape[2] != heads or t.shape[3] != d_h
+            or not t.is_contiguous()):
+        raise ValueError(f"{name}: expected contiguous {dtype} pages [n x rows x {heads} x {d_h}] on {device}")
+    return t.data_ptr()
+
+
+def lime_set_sequence(ctx: int, seq: lime_sequence) -> None:
+    _check(_lib().lime_set_sequence(ctx, ctypes.byref(seq)), "lime_set_sequence")
+
+
+def lime_sequence_workspace_bytes(ctx: int, B: int, rows: int) -> int:
+    return int(_lib().lime_sequence_workspace_bytes(ctx, B, rows))
+
+
+def lime_norm_rotate(ctx: int, seq: lime_sequence, q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], gamma_q: Optional[torch.Tensor],
+                     gamma_k: Optional[torch.Tensor], positions: Optional[torch.Tensor], q_out: torch.Tensor, k_out: Optional[torch.Tensor],
+                     cache_k: Optional[torch.Tensor] = None, cache_v: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+                     dev_flag: Optional[torch.Tensor] = None) -> None:
+    """cache_k, cache_v: pages [n x rows x Hkv x d_h]; slots count their rows, one page after the other."""
+    t, dev, n = q.dtype, q.device, q.shape[0]
+    (qp, qs), (kp, ks) = _rows(q, seq.Hq, seq.d_h, t, dev, "q"), _rows(k, seq.Hkv, seq.d_h, t, dev, "k", n)
+    vp, vs = _rows(v, seq.Hkv, seq.d_h, t, dev, "v", n)
+    (qo, qos), (ko, kos) = _rows(q_out, seq.Hq, seq.d_h, t, dev, "q_out", n), _rows(k_out, seq.Hkv, seq.d_h, t, dev, "k_out", n)
+    ck = None if cache_k is None else _pages(cache_k, seq.Hkv, seq.d_h, t, dev, "cache_k")
+    cv = None if cache_v is None else _pages(cache_v, seq.Hkv, seq.d_h, t, dev, "cache_v")
+    if cache_v is not None and cache_k is not None and cache_v.shape != cache_k.shape:
+        raise ValueError("cache_v: expected the shape of cache_k")
+    _check(_lib().lime_norm_rotate(ctx, qp, qs, kp, ks, vp, vs, _vector(gamma_q, seq.d_h, t, dev, "gamma_q"), _vector(gamma_k, seq.d_h, t, dev, "gamma_k"),
+                                   _ints(positions, dev, "positions", n), n, qo, qos, ko, kos, ck, cv,
+                                   0 if cache_k is None else cache_k.shape[0] * cache_k.shape[1], _ints(slots, dev, "slots", n),
+                                   _ints(dev_flag, dev, "dev_flag", 1), _stream()), "lime_norm_rotate")
+
+
+def lime_attend_history(ctx: int, seq: lime_sequence, q: torch.Tensor, off: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                        kv_off: Optional[torch.Tensor], out: torch.Tensor, ws: torch.Tensor) -> None:
+    t, dev = q.dtype, q.device
+    qp, qs = _rows(q, seq.Hq, seq.d_h, t, dev, "q")
+    (kp, ks), (vp, vs) = _rows(k, seq.Hkv, seq.d_h, t, dev, "k"), _rows(v, seq.Hkv, seq.d_h, t, dev, "v", k.shape[0])
+    op, os_ = _rows(out, seq.Hq, seq.d_h, t, dev, "out", q.shape[0])
+    B = _batch(off)
+    _check(_lib().lime_attend_history(ctx, qp, qs, _ints(off, dev, "off"), kp, ks, vp, vs, _ints(kv_off, dev, "kv_off", B + 1), B, q.shape[0],
+                                      k.shape[0], op, os_, _ptr(ws), ws.numel() * ws.element_size(), _stream()), "lime_attend_history")
+
+
+def lime_attend_tree(ctx: int, seq: lime_sequence, q: torch.Tensor, off: torch.Tensor, parent: Optional[torch.Tensor],
+                     tree_k: Optional[torch.Tensor], tree_v: Optional[torch.Tensor], cache_k: torch.Tensor, cache_v: torch.Tensor,
+                     page_table: torch.Tensor, ctx_len: torch.Tensor, dev_flag: Optional[torch.Tensor], out: torch.Tensor,
+                     ws: torch.Tensor) -> None:
+    t, dev, n = q.dtype, q.device, q.shape[0]
+    qp, qs = _rows(q, seq.Hq, seq.d_h, t, dev, "q")
+    (kp, ks), (vp, vs) = _rows(tree_k, seq.Hkv, seq.d_h, t, dev, "tree_k", n), _rows(tree_v, seq.Hkv, seq.d_h, t, dev, "tree_v", n)
+    op, os_ = _rows(out, seq.Hq, seq.d_h, t, dev, "out", n)
+    ck, cv = _pages(cache_k, seq.Hkv, seq.d_h, t, dev, "cache_k"), _pages(cache_v, seq.Hkv, seq.d_h, t, dev, "cache_v")
+    B = _batch(off)
+    if cache_v.shape != cache_k.shape:
+        raise ValueError("cache_v: expected the shape of cache_k")
+    if page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError(f"page_table: expected [{B} x pages]")
+    _check(_lib().lime_attend_tree(ctx, qp, qs, _ints(off, dev, "off"), _ints(parent, dev, "parent", n), kp, ks, vp, vs, B, n, ck, cv,
+                                   cache_k.shape[0], cache_k.shape[1], _ints(page_table, dev, "page_table"), page_table.shape[1],
+                                   _ints(ctx_len, dev, "ctx_len", B), _ints(dev_flag, dev, "dev_flag", 1), op, os_, _ptr(ws),
+                                   ws.numel() * ws.element_size(), _stream()), "lime_attend_tree")
+
+
+def _batch(off: torch.Tensor) -> int:
+    if not isinstance(off, torch.Tensor):
+        raise TypeError(f"expected a torch.Tensor, got {type(off).__name__}")
+    if off.dim() != 1 or off.numel() < 1:
+        raise ValueError("off: expected [users + 1]")
+    return off.numel() - 1
+
+
 def lime_precompute_candidate_links_noalloc(dtype: int, d: int, ell: int, cand_scale: float, links: torch.Tensor,
                                             cand_Wq: Optional[torch.Tensor], cand_Wk: Optional[torch.Tensor],
                                             cand_emb: torch.Tensor, out_w: torch.Tensor) -> None:
@@ -426,6 +549,42 @@ class _PlainCalls:
     def score_candidates_head(ctx, link_states, cand_w, cand_emb, C, cand_off, cand_ids, total, rows, flag, ws):
         return _PlainCalls._score(lime_score_candidates_head, ctx, link_states, cand_w, cand_emb, C, cand_off, cand_ids, total, rows, flag, ws)
 
+    @staticmethod
+    def _storage(t, bf16, name):
+        """q of a call of the sequence path: its type and device are the call's."""
+        if not _PlainCalls._tensor(t).is_cuda or t.dtype != (torch.bfloat16 if bf16 else torch.float32) or t.dim() != 3:
+            raise ValueError(f"{name}: expected CUDA rows of the context's type")
+        return t
+
+    @staticmethod
+    def norm_rotate(ctx, bf16, Hq, Hkv, d_h, q, k, v, gamma_q, gamma_k, positions, q_out, k_out, cache_k, cache_v, slots, flag, keep_k):
+        seq = lime_sequence(Hq, Hkv, d_h)
+        with torch.cuda.device(_PlainCalls._storage(q, bf16, "q").device):
+            if q_out is None:
+                q_out = q.new_empty((q.shape[0], Hq, d_h))
+            if k_out is None and (cache_k is None or keep_k):
+                k_out = q.new_empty((q.shape[0], Hkv, d_h))
+            lime_norm_rotate(ctx, seq, q, k, v, gamma_q, gamma_k, positions, q_out, k_out, cache_k, cache_v, slots, flag)
+        return q_out, k_out
+
+    @staticmethod
+    def attend_history(ctx, bf16, Hq, Hkv, d_h, q, off, k, v, kv_off, out):
+        seq = lime_sequence(Hq, Hkv, d_h)
+        with torch.cuda.device(_PlainCalls._storage(q, bf16, "q").device):
+            out = q.new_empty((q.shape[0], Hq, d_h)) if out is None else out
+            ws = torch.empty(lime_sequence_workspace_bytes(ctx, _batch(off), q.shape[0]), dtype=torch.uint8, device=q.device)
+            lime_attend_history(ctx, seq, q, off, _PlainCalls._tensor(k), v, kv_off, out, ws)
+        return out
+
+    @staticmethod
+    def attend_tree(ctx, bf16, Hq, Hkv, d_h, q, off, parent, tree_k, tree_v, cache_k, cache_v, page_table, ctx_len, flag, out):
+        seq = lime_sequence(Hq, Hkv, d_h)
+        with torch.cuda.device(_PlainCalls._storage(q, bf16, "q").device):
+            out = q.new_empty((q.shape[0], Hq, d_h)) if out is None else out
+            ws = torch.empty(lime_sequence_workspace_bytes(ctx, _batch(off), q.shape[0]), dtype=torch.uint8, device=q.device)
+            lime_attend_tree(ctx, seq, q, off, parent, tree_k, tree_v, cache_k, cache_v, _PlainCalls._tensor(page_table), ctx_len, flag, out, ws)
+        return out
+
 
 # ----------------------------------------------------------------------------- convenience wrapper
 class Lime:
@@ -445,6 +604,7 @@ class Lime:
         self._ws = None
         self._ws_for = None             # (B, total_tokens) that _ws is known to serve
         self._head_ws = None
+        self._seq = None                # (bf16, Hq, Hkv, d_h) of the sequence path
 
     def close(self):
         if self.ctx:
@@ -547,3 +707,37 @@ class Lime:
             self._head_ws = torch.empty(need, dtype=torch.uint8, device=link_states.device)
         return self._native.score_candidates_head(self.ctx, link_states, cand_w, cand_emb, C, cand_off, cand_ids, total_cands, corpus_rows,
                                                   dev_flag, self._head_ws)
+
+    # ---- the sequence path: attention over whole histories, with a cache of keys and values (for inference: no gradients are kept)
+    def set_sequence(self, Hq: int, Hkv: int, d_h: int, attn_scale: float = 0.0, norm_eps: float = 0.0, rot_dim: int = 0,
+                     rot_interleaved: bool = False, rot_base: float = 0.0) -> None:
+        lime_set_sequence(self.ctx, lime_sequence(Hq, Hkv, d_h, attn_scale, norm_eps, rot_dim, int(rot_interleaved), rot_base))
+        self._seq = (self.tdtype == torch.bfloat16, Hq, Hkv, d_h)
+
+    def _sequence(self):
+        if self._seq is None:
+            raise LimeError(5, "set_sequence has not been called")
+        return self._seq
+
+    def norm_rotate(self, q: torch.Tensor, k: torch.Tensor, positions: Optional[torch.Tensor], v: Optional[torch.Tensor] = None,
+                    gamma_q: Optional[torch.Tensor] = None, gamma_k: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                    k_out: Optional[torch.Tensor] = None, cache_k: Optional[torch.Tensor] = None, cache_v: Optional[torch.Tensor] = None,
+                    slots: Optional[torch.Tensor] = None, dev_flag: Optional[torch.Tensor] = None, keep_k: bool = False):
+        """Returns (q, k) normed and rotated, in q_out and k_out or in new tensors; with a cache, keys (and v) go to its rows `slots`, and
+        k is None unless k_out is given or keep_k set."""
+        return self._native.norm_rotate(self.ctx, *self._sequence(), q, k, v, gamma_q, gamma_k, positions, q_out, k_out, cache_k, cache_v, slots,
+                                        dev_flag, keep_k)
+
+    def attend_history(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, off: torch.Tensor, kv_off: Optional[torch.Tensor] = None,
+                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Causal attention over packed histories.  The scratch is a tensor of the call's own, so calls may overlap on several streams
+        and in captured graphs.  Rows past the last history are left unwritten (whatever a new `out` happens to hold)."""
+        return self._native.attend_history(self.ctx, *self._sequence(), q, off, k, v, kv_off, out)
+
+    def attend_tree(self, q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tensor, page_table: torch.Tensor, ctx_len: torch.Tensor,
+                    off: torch.Tensor, parent: Optional[torch.Tensor] = None, tree_k: Optional[torch.Tensor] = None,
+                    tree_v: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                    dev_flag: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """A few rows per user over the cached history and, with tree_k and tree_v, over themselves and their ancestors."""
+        return self._native.attend_tree(self.ctx, *self._sequence(), q, off, parent, tree_k, tree_v, cache_k, cache_v, page_table, ctx_len,
+                                        dev_flag, out)

@@ -1,0 +1,254 @@
+// Attention of the sequence path on CUDA cores:
+//
+//   out_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(scale log2(e) <q_i, k_j> - m_i)   over the keys j that row i sees
+//
+// One block of 256 threads per work item (seq_common.cuh) and head of keys: RT stacked query rows against tiles of 64 keys, all in fp32
+// (FFMA), running maximum and sum per row, one pass over keys and values.  Threads are 16 x 16: thread (ty, tx) forms the scores of rows
+// ty, ty + 16, .. with keys tx, tx + 16, .., and owns 16 / VW-wide column groups of the same rows' results, so maxima and sums stay
+// within half a warp and the probabilities pass through shared memory without a block barrier.  The next tile's keys and values are
+// copied (cp.async) while a tile is worked on.
+// A masked position is -1 among the probabilities of a tile that has one: its value row is then not touched at all, so that infinities
+// and NaN there stay there.
+#include <type_traits>
+
+#include "seq_common.cuh"
+#include "tc_common.cuh"
+
+namespace lime {
+
+constexpr int kSimtKeys = 64;
+
+template <int DHP, int RT>
+struct SimtCfg {
+  static constexpr int LD = DHP + 4, PLD = kSimtKeys + 4;
+  static constexpr int VW = DHP >= 64 ? 4 : 2, DC = DHP / (16 * VW), RI = RT / 16;
+  static constexpr int OFF_K = RT * LD, OFF_V = OFF_K + 2 * kSimtKeys * LD, OFF_P = OFF_V + 2 * kSimtKeys * LD;
+  static constexpr int OFF_MASK = OFF_P + RT * PLD;                               // [2 tile parities][RT] of two words
+  static constexpr int SMEM = (OFF_MASK + 4 * RT) * 4;
+  static_assert(SMEM <= 232448, "shared memory of one block");
+};
+
+__device__ __forceinline__ void cp_async16(void* dst, const void* src, bool there) {
+  const int n = there ? 16 : 0;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(dst)), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void seq_copy4(float* dst, const float* src, bool there) { cp_async16(dst, src, there); }
+__device__ __forceinline__ void seq_copy4(float* dst, const __nv_bfloat16* src, bool there) {
+  float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (there) {
+    const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
+    f.x = __uint_as_float(w.x << 16); f.y = __uint_as_float(w.x & 0xffff0000u);
+    f.z = __uint_as_float(w.y << 16); f.w = __uint_as_float(w.y & 0xffff0000u);
+  }
+  *reinterpret_cast<float4*>(dst) = f;
+}
+
+template <typename T, int DHP, int RT, bool TREE>
+__global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
+  using C = SimtCfg<DHP, RT>;
+  constexpr int LD = C::LD, PLD = C::PLD, KT = kSimtKeys, VW = C::VW, DC = C::DC, RI = C::RI;
+  extern __shared__ __align__(16) float sm[];
+  float* sQ = sm; float* sK = sm + C::OFF_K; float* sV = sm + C::OFF_V; float* sP = sm + C::OFF_P;
+  uint32_t* sMask = reinterpret_cast<uint32_t*>(sm + C::OFF_MASK);
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int idx = (int)blockIdx.x / p.Hkv, kvh = (int)blockIdx.x % p.Hkv;
+  if (idx >= p.plan->n_items) return;
+  const SeqItem it = p.items[idx];
+  const int G = p.G, rows = it.rows * G, n_tree = TREE ? seq_tree_tiles(p, it) : 0, chunks = p.dh / 4;
+  // queries: rows and columns that are not there are zeros
+  for (int i = tid; i < RT * (DHP / 4); i += 256) {
+    const int r = i / (DHP / 4), c = i % (DHP / 4);
+    const bool there = r < rows && c < chunks;
+    const T* src = static_cast<const T*>(p.q) + (there ? (int64_t)(it.row0 + r / G) * p.q_stride + (kvh * G + r % G) * p.dh + c * 4 : 0);
+    seq_copy4(sQ + r * LD + c * 4, src, there);
+  }
+  auto fetch = [&](int t, int buf) {
+    const SeqTile s = seq_tile<TREE>(p, it, n_tree, t);
+    for (int i = tid; i < KT * (DHP / 4); i += 256) {
+      const int j = i / (DHP / 4), c = i % (DHP / 4);
+      bool there = s.j0 + j < s.n && c < chunks;
+      const T *kp = static_cast<const T*>(TREE ? p.q : p.k), *vp = kp;
+      if (there) {
+        if (!TREE || s.kind == 2) {
+          const int64_t row = (int64_t)(TREE ? it.row0 - it.c : it.a) + s.j0 + j;
+          kp = static_cast<const T*>(p.k) + row * p.k_stride + kvh * p.dh + c * 4;
+          vp = static_cast<const T*>(p.v) + row * p.v_stride + kvh * p.dh + c * 4;
+        } else {
+          const int64_t pg = seq_page(p, it.a, s.j0 + j);
+          there = pg < p.n_pages;
+          if (there) {
+            const int64_t row = (pg * p.page_rows + ((s.j0 + j) & (p.page_rows - 1))) * p.Hkv + kvh;
+            kp = static_cast<const T*>(p.ck) + row * p.dh + c * 4;
+            vp = static_cast<const T*>(p.cv) + row * p.dh + c * 4;
+          }
+        }
+      }
+      seq_copy4(sK + (buf * KT + j) * LD + c * 4, kp, there);
+      seq_copy4(sV + (buf * KT + j) * LD + c * 4, vp, there);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  float m[RI], l[RI], acc[RI][DC * VW];
+#pragma unroll
+  for (int i = 0; i < RI; ++i) {
+    m[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < DC * VW; ++c) acc[i][c] = 0.f;
+  }
+  // the row whose mask this thread keeps: its token, and how far up its chain of ancestors it has come
+  const int mtok = tid < rows ? tid / G : 0;
+  int anc = it.c + mtok;
+  if (it.t0 < it.t1) fetch(it.t0, 0);
+  for (int t = it.t0; t < it.t1; ++t) {
+    const int buf = (t - it.t0) & 1;
+    const SeqTile s = seq_tile<TREE>(p, it, n_tree, t);
+    const bool masked = s.kind == 2 || (s.kind == 0 ? s.j0 + KT > it.c : s.j0 + KT > s.n);
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    uint32_t* mask = sMask + buf * 2 * RT;           // a slower warp may still read the previous tile's
+    if (masked && tid < RT) {
+      uint32_t w0 = 0, w1 = 0;
+      if (TREE && s.kind == 2) {
+        while (anc >= s.j0) {
+          const int bit = anc - s.j0;
+          if (bit < 32) w0 |= 1u << bit; else if (bit < 64) w1 |= 1u << (bit - 32);
+          anc = seq_parent(p, it.row0 - it.c, anc);
+        }
+      } else {
+        const int n = (s.kind == 0 ? it.c + mtok : s.n) - s.j0;               // of the tile's keys
+        w0 = n >= 32 ? 0xffffffffu : n > 0 ? (1u << n) - 1u : 0u;
+        w1 = n >= 64 ? 0xffffffffu : n > 32 ? (1u << (n - 32)) - 1u : 0u;
+      }
+      mask[2 * tid] = w0; mask[2 * tid + 1] = w1;
+    }
+    __syncthreads();
+    if (t + 1 < it.t1) fetch(t + 1, buf ^ 1);
+    const float *kb = sK + buf * KT * LD, *vb = sV + buf * KT * LD;
+    float sc[RI][4];
+#pragma unroll
+    for (int i = 0; i < RI; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sc[i][j] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < DHP; c += 4) {
+      float4 kf[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) kf[j] = *reinterpret_cast<const float4*>(kb + (tx + 16 * j) * LD + c);
+#pragma unroll
+      for (int i = 0; i < RI; ++i) {
+        const float4 qf = *reinterpret_cast<const float4*>(sQ + (ty + 16 * i) * LD + c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          sc[i][j] = fmaf(qf.x, kf[j].x, sc[i][j]); sc[i][j] = fmaf(qf.y, kf[j].y, sc[i][j]);
+          sc[i][j] = fmaf(qf.z, kf[j].z, sc[i][j]); sc[i][j] = fmaf(qf.w, kf[j].w, sc[i][j]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < RI; ++i) {
+      const int r = ty + 16 * i;
+      bool sees[4];
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sees[j] = !masked || ((mask[2 * r + (j >> 1)] >> (tx + 16 * (j & 1))) & 1u) != 0;
+        sc[i][j] = sees[j] ? sc[i][j] * p.scale_log2 : -INFINITY;
+        mx = fmaxf(mx, sc[i][j]);
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      const float m_new = fmaxf(m[i], mx), ref = m_new == -INFINITY ? 0.f : m_new;
+      const float factor = exp2f(m[i] - ref);
+      m[i] = m_new;
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float e = exp2f(sc[i][j] - ref);
+        if (sees[j]) sum += e;
+        sP[r * PLD + tx + 16 * j] = sees[j] ? e : -1.f;
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      l[i] = l[i] * factor + sum;
+#pragma unroll
+      for (int c = 0; c < DC * VW; ++c) acc[i][c] *= factor;
+    }
+    __syncwarp();                                    // a row's probabilities come from the half warp that reads them
+    auto values = [&](auto skip) {
+#pragma unroll 2
+      for (int j = 0; j < KT; j += 4) {
+        float pf[RI][4];
+#pragma unroll
+        for (int i = 0; i < RI; ++i) *reinterpret_cast<float4*>(pf[i]) = *reinterpret_cast<const float4*>(sP + (ty + 16 * i) * PLD + j);
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) {
+          float vf[DC * VW];
+#pragma unroll
+          for (int c = 0; c < DC; ++c) {
+            const float* src = vb + (j + jj) * LD + c * 16 * VW + tx * VW;
+            if constexpr (VW == 4) *reinterpret_cast<float4*>(vf + c * VW) = *reinterpret_cast<const float4*>(src);
+            else *reinterpret_cast<float2*>(vf + c * VW) = *reinterpret_cast<const float2*>(src);
+          }
+#pragma unroll
+          for (int i = 0; i < RI; ++i)
+            if (!decltype(skip)::value || !(pf[i][jj] < 0.f)) {
+#pragma unroll
+              for (int c = 0; c < DC * VW; ++c) acc[i][c] = fmaf(pf[i][jj], vf[c], acc[i][c]);
+            }
+        }
+      }
+    };
+    if (masked) values(std::true_type()); else values(std::false_type());
+    __syncwarp();
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < RI; ++i) {
+    const int r = ty + 16 * i;
+    if (r >= rows) continue;
+    if (it.part < 0) {
+      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+      T* o = static_cast<T*>(p.out) + (int64_t)(it.row0 + r / G) * p.out_stride + (kvh * G + r % G) * p.dh;
+#pragma unroll
+      for (int c = 0; c < DC; ++c)
+        if (c * 16 * VW + tx * VW < p.dh)
+#pragma unroll
+          for (int e = 0; e < VW; ++e) Store<T>::st(o + c * 16 * VW + tx * VW + e, acc[i][c * VW + e] * inv);
+    } else {
+      const int R = p.tok * G;
+      const int64_t at = (int64_t)it.part * p.Hkv + kvh;
+      if (tx == 0) { p.part_ml[at * 2 * R + r] = m[i]; p.part_ml[(at * 2 + 1) * R + r] = l[i]; }
+      float* o = p.part_acc + (at * R + r) * p.dh;
+#pragma unroll
+      for (int c = 0; c < DC; ++c)
+        if (c * 16 * VW + tx * VW < p.dh)
+#pragma unroll
+          for (int e = 0; e < VW; ++e) o[c * 16 * VW + tx * VW + e] = acc[i][c * VW + e];
+    }
+  }
+}
+
+template <typename T, int DHP, int RT, bool TREE>
+static lime_status launch_simt(const SeqParams& p, cudaStream_t st) {
+  static bool set[kMaxDeviceOrdinals] = {};
+  constexpr int smem = SimtCfg<DHP, RT>::SMEM;
+  const lime_status s = ensure_dynamic_smem((const void*)k_seq_attn_simt<T, DHP, RT, TREE>, smem, set);
+  if (s != LIME_OK) return s;
+  ProfScope _p("k_seq_attn_simt", st);
+  launch_pdl(k_seq_attn_simt<T, DHP, RT, TREE>, dim3((unsigned)p.items_upper * p.Hkv), dim3(256), smem, st, p);
+  LIME_LAUNCH_CHECK("k_seq_attn_simt");
+  return LIME_OK;
+}
+template <typename T, int DHP>
+static lime_status pick_simt(const SeqParams& p, bool tree, bool few, cudaStream_t st) {
+  if (few) return tree ? launch_simt<T, DHP, 16, true>(p, st) : launch_simt<T, DHP, 16, false>(p, st);
+  return tree ? launch_simt<T, DHP, 64, true>(p, st) : launch_simt<T, DHP, 64, false>(p, st);
+}
+lime_status launch_seq_attn_simt(const SeqParams& p, int dtype, bool tree, bool few, cudaStream_t st) {
+  if (dtype == LIME_BF16)
+    return p.dh <= 32 ? pick_simt<__nv_bfloat16, 32>(p, tree, few, st) : p.dh <= 64 ? pick_simt<__nv_bfloat16, 64>(p, tree, few, st) : pick_simt<__nv_bfloat16, 128>(p, tree, few, st);
+  return p.dh <= 32 ? pick_simt<float, 32>(p, tree, few, st) : p.dh <= 64 ? pick_simt<float, 64>(p, tree, few, st) : pick_simt<float, 128>(p, tree, few, st);
+}
+
+}  // namespace lime

@@ -616,6 +616,7 @@ lime_status lime_create(const lime_config* cfg, lime_ctx** out) {
   c->ln_eps = g.ln_eps > 0.f ? g.ln_eps : 1e-5f;
   c->keff = nullptr; c->keff_hl = nullptr; c->links32 = nullptr; c->dev_err = nullptr;
   c->have_head = c->have_ctx_mlp = false; c->ctx_dc = 0;
+  c->have_seq = false;
   c->head_W1bT = nullptr; c->head_W1aT = nullptr; c->head_w2 = nullptr; c->ctx_first = nullptr;
   c->tc_mode = tensor_core_mode(g, d_ff);
   c->side256 = c->tc_mode == 2 && link_side_d256_supported(g.d, d_ff, g.H, g.ell);

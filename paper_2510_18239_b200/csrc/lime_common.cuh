@@ -124,6 +124,9 @@ struct Ctx {
   int* dev_err;     // device word: 0, or the code of the first bounded wait that gave up in a kernel of this context
   float attn_scale, cand_scale, ln_eps;
   int d_ff, d_h;
+  bool have_seq;              // lime_set_sequence (seq_api.cu)
+  lime_sequence seq;          // as given, zeros replaced by what they mean
+  uint64_t rot_freq[64];      // pair i of the rotation: turns per position, as a fraction of 2^64
 };
 
 // record a CUDA error for lime_last_cuda_error(); returns LIME_CUDA_ERROR
