@@ -1,4 +1,4 @@
-// Attention of the sequence path on CUDA cores:
+// Attention of the sequence path on CUDA cores (fp32):
 //
 //   out_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(scale log2(e) <q_i, k_j> - m_i)   over the keys j that row i sees
 //
@@ -32,18 +32,7 @@ __device__ __forceinline__ void cp_async16(void* dst, const void* src, bool ther
   const int n = there ? 16 : 0;
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(dst)), "l"(src), "r"(n) : "memory");
 }
-__device__ __forceinline__ void seq_copy4(float* dst, const float* src, bool there) { cp_async16(dst, src, there); }
-__device__ __forceinline__ void seq_copy4(float* dst, const __nv_bfloat16* src, bool there) {
-  float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (there) {
-    const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
-    f.x = __uint_as_float(w.x << 16); f.y = __uint_as_float(w.x & 0xffff0000u);
-    f.z = __uint_as_float(w.y << 16); f.w = __uint_as_float(w.y & 0xffff0000u);
-  }
-  *reinterpret_cast<float4*>(dst) = f;
-}
-
-template <typename T, int DHP, int RT, bool TREE>
+template <int DHP, int RT, bool TREE>
 __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
   using C = SimtCfg<DHP, RT>;
   constexpr int LD = C::LD, PLD = C::PLD, KT = kSimtKeys, VW = C::VW, DC = C::DC, RI = C::RI;
@@ -61,32 +50,32 @@ __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
   for (int i = tid; i < RT * (DHP / 4); i += 256) {
     const int r = i / (DHP / 4), c = i % (DHP / 4);
     const bool there = r < rows && c < chunks;
-    const T* src = static_cast<const T*>(p.q) + (there ? (int64_t)(it.row0 + r / G) * p.q_stride + (kvh * G + r % G) * p.dh + c * 4 : 0);
-    seq_copy4(sQ + r * LD + c * 4, src, there);
+    const float* src = static_cast<const float*>(p.q) + (there ? (int64_t)(it.row0 + r / G) * p.q_stride + (kvh * G + r % G) * p.dh + c * 4 : 0);
+    cp_async16(sQ + r * LD + c * 4, src, there);
   }
   auto fetch = [&](int t, int buf) {
     const SeqTile s = seq_tile<TREE>(p, it, n_tree, t);
     for (int i = tid; i < KT * (DHP / 4); i += 256) {
       const int j = i / (DHP / 4), c = i % (DHP / 4);
       bool there = s.j0 + j < s.n && c < chunks;
-      const T *kp = static_cast<const T*>(TREE ? p.q : p.k), *vp = kp;
+      const float *kp = static_cast<const float*>(TREE ? p.q : p.k), *vp = kp;
       if (there) {
         if (!TREE || s.kind == 2) {
           const int64_t row = (int64_t)(TREE ? it.row0 - it.c : it.a) + s.j0 + j;
-          kp = static_cast<const T*>(p.k) + row * p.k_stride + kvh * p.dh + c * 4;
-          vp = static_cast<const T*>(p.v) + row * p.v_stride + kvh * p.dh + c * 4;
+          kp = static_cast<const float*>(p.k) + row * p.k_stride + kvh * p.dh + c * 4;
+          vp = static_cast<const float*>(p.v) + row * p.v_stride + kvh * p.dh + c * 4;
         } else {
           const int64_t pg = seq_page(p, it.a, s.j0 + j);
           there = pg < p.n_pages;
           if (there) {
             const int64_t row = (pg * p.page_rows + ((s.j0 + j) & (p.page_rows - 1))) * p.Hkv + kvh;
-            kp = static_cast<const T*>(p.ck) + row * p.dh + c * 4;
-            vp = static_cast<const T*>(p.cv) + row * p.dh + c * 4;
+            kp = static_cast<const float*>(p.ck) + row * p.dh + c * 4;
+            vp = static_cast<const float*>(p.cv) + row * p.dh + c * 4;
           }
         }
       }
-      seq_copy4(sK + (buf * KT + j) * LD + c * 4, kp, there);
-      seq_copy4(sV + (buf * KT + j) * LD + c * 4, vp, there);
+      cp_async16(sK + (buf * KT + j) * LD + c * 4, kp, there);
+      cp_async16(sV + (buf * KT + j) * LD + c * 4, vp, there);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -209,12 +198,12 @@ __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
     if (r >= rows) continue;
     if (it.part < 0) {
       const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
-      T* o = static_cast<T*>(p.out) + (int64_t)(it.row0 + r / G) * p.out_stride + (kvh * G + r % G) * p.dh;
+      float* o = static_cast<float*>(p.out) + (int64_t)(it.row0 + r / G) * p.out_stride + (kvh * G + r % G) * p.dh;
 #pragma unroll
       for (int c = 0; c < DC; ++c)
         if (c * 16 * VW + tx * VW < p.dh)
 #pragma unroll
-          for (int e = 0; e < VW; ++e) Store<T>::st(o + c * 16 * VW + tx * VW + e, acc[i][c * VW + e] * inv);
+          for (int e = 0; e < VW; ++e) o[c * 16 * VW + tx * VW + e] = acc[i][c * VW + e] * inv;
     } else {
       const int R = p.tok * G;
       const int64_t at = (int64_t)it.part * p.Hkv + kvh;
@@ -229,26 +218,24 @@ __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
   }
 }
 
-template <typename T, int DHP, int RT, bool TREE>
+template <int DHP, int RT, bool TREE>
 static lime_status launch_simt(const SeqParams& p, cudaStream_t st) {
   static bool set[kMaxDeviceOrdinals] = {};
   constexpr int smem = SimtCfg<DHP, RT>::SMEM;
-  const lime_status s = ensure_dynamic_smem((const void*)k_seq_attn_simt<T, DHP, RT, TREE>, smem, set);
+  const lime_status s = ensure_dynamic_smem((const void*)k_seq_attn_simt<DHP, RT, TREE>, smem, set);
   if (s != LIME_OK) return s;
   ProfScope _p("k_seq_attn_simt", st);
-  launch_pdl(k_seq_attn_simt<T, DHP, RT, TREE>, dim3((unsigned)p.items_upper * p.Hkv), dim3(256), smem, st, p);
+  launch_pdl(k_seq_attn_simt<DHP, RT, TREE>, dim3((unsigned)p.items_upper * p.Hkv), dim3(256), smem, st, p);
   LIME_LAUNCH_CHECK("k_seq_attn_simt");
   return LIME_OK;
 }
-template <typename T, int DHP>
+template <int DHP>
 static lime_status pick_simt(const SeqParams& p, bool tree, bool few, cudaStream_t st) {
-  if (few) return tree ? launch_simt<T, DHP, 16, true>(p, st) : launch_simt<T, DHP, 16, false>(p, st);
-  return tree ? launch_simt<T, DHP, 64, true>(p, st) : launch_simt<T, DHP, 64, false>(p, st);
+  if (few) return tree ? launch_simt<DHP, 16, true>(p, st) : launch_simt<DHP, 16, false>(p, st);
+  return tree ? launch_simt<DHP, 64, true>(p, st) : launch_simt<DHP, 64, false>(p, st);
 }
-lime_status launch_seq_attn_simt(const SeqParams& p, int dtype, bool tree, bool few, cudaStream_t st) {
-  if (dtype == LIME_BF16)
-    return p.dh <= 32 ? pick_simt<__nv_bfloat16, 32>(p, tree, few, st) : p.dh <= 64 ? pick_simt<__nv_bfloat16, 64>(p, tree, few, st) : pick_simt<__nv_bfloat16, 128>(p, tree, few, st);
-  return p.dh <= 32 ? pick_simt<float, 32>(p, tree, few, st) : p.dh <= 64 ? pick_simt<float, 64>(p, tree, few, st) : pick_simt<float, 128>(p, tree, few, st);
+lime_status launch_seq_attn_simt(const SeqParams& p, bool tree, bool few, cudaStream_t st) {
+  return p.dh <= 32 ? pick_simt<32>(p, tree, few, st) : p.dh <= 64 ? pick_simt<64>(p, tree, few, st) : pick_simt<128>(p, tree, few, st);
 }
 
 }  // namespace lime

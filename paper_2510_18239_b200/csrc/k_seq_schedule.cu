@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kSeqThreads) k_seq_schedule(const SeqParams p)
     }
   }
   __syncthreads();
-  if (tid == 0) { p.plan->n_items = s_items; p.plan->n_split = s_split; p.plan->n_parts = s_parts; }
+  if (tid == 0) { p.plan->n_items = s_items; p.plan->n_split = s_split; p.plan->n_parts = s_parts; p.plan->taken = 0; }
 }
 
 lime_status launch_seq_schedule(const SeqParams& p, bool tree, cudaStream_t st) {

@@ -25,6 +25,15 @@ struct SeqTiling { int tok, kt, chunk_min, chunk_target; bool few; };
 static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows) {
   const int G = c->seq.Hq / c->seq.Hkv;
   SeqTiling t;
+  if (c->cfg.dtype == LIME_BF16) {
+    // tensor cores: two slots of 128 stacked rows
+    t.few = false;
+    t.tok = 2 * (128 / G);
+    t.kt = 128;
+    t.chunk_min = 8;
+    t.chunk_target = 3 * kSMs;
+    return t;
+  }
   // CUDA cores: 64 stacked rows a tile, or 16 where a user has no more on average
   t.few = G <= 16 && rows * G <= 16ll * B;
   t.tok = (t.few ? 16 : 64) / G;
@@ -79,7 +88,8 @@ static lime_status attend(const Ctx* c, SeqParams& p, bool tree, void* ws, size_
   if ((int64_t)p.items_upper * p.Hkv > 0x7fffffffLL) return LIME_UNSUPPORTED_SHAPE;
   lime_status s;
   if ((s = launch_seq_schedule(p, tree, st)) != LIME_OK) return s;
-  if ((s = launch_seq_attn_simt(p, c->cfg.dtype, tree, tiling(c, p.B, p.q_rows).few, st)) != LIME_OK) return s;
+  s = c->cfg.dtype == LIME_BF16 ? launch_seq_attn_tc(p, tree, st) : launch_seq_attn_simt(p, tree, tiling(c, p.B, p.q_rows).few, st);
+  if (s != LIME_OK) return s;
   return may_split ? launch_seq_merge(p, c->cfg.dtype, st) : LIME_OK;
 }
 

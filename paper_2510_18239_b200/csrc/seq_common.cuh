@@ -23,7 +23,7 @@ struct SeqItem {
   int32_t part;           // where the partial result goes; -1: the item is the whole row tile
 };
 struct SeqSplit { int32_t row0, rows, part0, n; };       // a row tile cut into n items, parts part0 ..
-struct SeqPlan { int32_t n_items, n_split, n_parts, pad; };
+struct SeqPlan { int32_t n_items, n_split, n_parts, taken; };     // taken: items fetched beyond the first of every CTA
 
 struct SeqParams {
   const void *q, *k, *v;                 // history: k, v the packed keys; tree: the new rows' (nullable)
@@ -100,6 +100,7 @@ struct NormRotateArgs {
 lime_status launch_norm_rotate(const NormRotateArgs& a, cudaStream_t st);
 lime_status launch_seq_schedule(const SeqParams& p, bool tree, cudaStream_t st);
 lime_status launch_seq_merge(const SeqParams& p, int dtype, cudaStream_t st);
-lime_status launch_seq_attn_simt(const SeqParams& p, int dtype, bool tree, bool few_rows, cudaStream_t st);
+lime_status launch_seq_attn_tc(const SeqParams& p, bool tree, cudaStream_t st);        // bf16
+lime_status launch_seq_attn_simt(const SeqParams& p, bool tree, bool few_rows, cudaStream_t st);                    // fp32
 
 }  // namespace lime

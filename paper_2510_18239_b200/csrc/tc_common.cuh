@@ -323,6 +323,10 @@ bool make_tmap_bf16_sw128(CUtensorMap* out, const void* base, uint64_t rows, uin
 // box_cols * 2 bytes apart under the swizzle of that span (what make_sdesc_k_sw describes).
 bool make_tmap_bf16_kmajor(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch_elems,
                            uint32_t box_rows, uint32_t box_cols);
+// Rows of heads [rows x heads x d_h] bf16, row pitch `pitch_elems`, box [box_rows x box_heads x 64 features], 128-byte swizzle: the box's
+// (row, head) pairs land as consecutive 128-byte rows, features past d_h as zeros.
+bool make_tmap_bf16_heads(CUtensorMap* out, const void* base, uint32_t heads, uint32_t d_h, uint64_t rows, uint64_t pitch_elems,
+                          uint32_t box_heads, uint32_t box_rows);
 // Kernels that need more than 48 KB of dynamic shared memory must have the limit raised once per device; `done` is
 // the caller's per-kernel record (one flag per device ordinal).
 constexpr int kMaxDeviceOrdinals = 64;

@@ -57,6 +57,20 @@ bool make_tmap_bf16_kmajor(CUtensorMap* out, const void* base, uint64_t rows, ui
             CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_tmap_bf16_heads(CUtensorMap* out, const void* base, uint32_t heads, uint32_t d_h, uint64_t rows, uint64_t pitch_elems,
+                          uint32_t box_heads, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn || rows == 0 || heads == 0 || d_h == 0 || box_heads == 0 || box_heads > 256 || box_rows == 0 || box_rows > 256) return false;
+  if ((reinterpret_cast<uintptr_t>(base) & 15u) || (d_h * 2) % 16 || (pitch_elems * 2) % 16) return false;
+  const cuuint64_t gdim[3] = {d_h, heads, rows};
+  const cuuint64_t gstride[2] = {(cuuint64_t)d_h * 2, pitch_elems * 2};
+  const cuuint32_t box[3] = {64, box_heads, box_rows};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), gdim, gstride, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool pdl_enabled() {
   static const bool on = [] {
     const char* e = std::getenv("LIME_PDL");
