@@ -2,16 +2,19 @@
 //
 //   out_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(scale log2(e) (<q_i, k_j> - m_i))   over the keys j that row i sees
 //
-// A persistent CTA per SM takes the work items of k_seq_schedule one after the other (a counter deals them, the longest first).  An item
-// is up to two slots of 128 stacked rows (tokens x the query heads of one head of keys) against key tiles of 128:
+// A persistent CTA per SM walks its share of the work items of k_seq_schedule (dealt in their order, back and forth, so the longest come
+// first and rounds even out).  An item is up to two slots of 128 stacked rows (tokens x the query heads of one head of keys) against key
+// tiles of 128:
 //   scores [128 x 128] = Q [128 x d_h] . K_tile^T      both operands from shared memory, where TMA leaves them 128-byte swizzled
 //   O [128 x d_h]     += P [128 x 128] . V_tile        P as bf16 in tensor memory, over its own scores; V as it lies (MN-major)
 // Two slots because one alone is a chain (scores, softmax, values) several times its tensor time: while the softmax warps of one work,
 // the pipe works for the other.  An item of no more than 128 rows puts the same rows into both slots, which take the key tiles in turn
 // and are joined in the end; so a single new event streams its cache through two chains.
-//  * Warp 0 loads (one lane a page where keys lie in pages), warp 1 issues the scores, warp 2 the values, warp 3 mends value tiles (below)
-//    and fetches items; warps 4..7 and 8..11 are the softmax of a slot, one thread per row.  Online softmax with lazy rescale: the
-//    reference maximum is raised only when exceeded by 2^8.
+//  * Warp 0 loads (one lane a page where keys lie in pages), warp 1 issues the scores, warp 2 the values, warp 3 mends value tiles (below);
+//    warps 4..7 and 8..11 are the softmax of a slot, one thread per row.  Online softmax with lazy rescale: the reference maximum is
+//    raised only when exceeded by 2^8.
+//  * Nothing waits for the end of an item but what needs it: the next one's keys and queries are loaded and its first scores formed while
+//    the softmax warps write a result out (100 users of 0..1000 rows, 4 heads of 32: LIME_TODO us with a barrier of the CTA between items).
 //  * d_h that is not 64 or 128: TMA fills the columns that are not there with zeros in shared memory only, and the contractions stop at
 //    the next multiple of 16.
 //  * Probabilities are rounded to bf16 for the value product (the operands of one tcgen05.mma have one type); the row sum is taken of the
@@ -26,13 +29,15 @@ namespace lime {
 
 template <int DHP_>
 struct SeqTcCfg {
-  static constexpr int DHP = DHP_, KT = 128, THREADS = 384, STAGES = DHP == 128 ? 5 : 10;
+  static constexpr int DHP = DHP_, THREADS = 384, STAGES = DHP == 128 ? 5 : 10, QBUFS = DHP == 128 ? 1 : 2;
   static constexpr uint32_t SUB = 128 * 128;                       // [128 rows x 64 features]
   static constexpr uint32_t TILE = (DHP / 64) * SUB;
-  static constexpr uint32_t OFF_Q = 0, OFF_KV = 2 * TILE, OFF_ML = OFF_KV + STAGES * TILE, OFF_BAR = OFF_ML + 4 * 128 * 4;
-  static constexpr uint32_t SMEM = OFF_BAR + 512;
+  static constexpr uint32_t OFF_Q = 0, OFF_KV = QBUFS * 2 * TILE, OFF_BAR = OFF_KV + STAGES * TILE;
+  static constexpr uint32_t OFF_ML = OFF_BAR + 512;               // references and sums of joined slots: [2 slots][128] pairs
+  static constexpr uint32_t OFF_BAD = OFF_ML + 2 * 128 * 8;       // a bit for every item of the CTA
+  static constexpr uint32_t SMEM = OFF_BAD + 512;
   static constexpr uint32_t COL_S = 0, COL_O = 256;                // scores: two of 128 columns; accumulators: two of DHP
-  static constexpr int REGS_LAUNCH = 168, REGS_CONTROL = 88, REGS_SOFTMAX = 208;
+  static constexpr int REGS_LAUNCH = 168, REGS_CONTROL = 56, REGS_SOFTMAX = 224;
   static_assert(128 * REGS_CONTROL + 256 * REGS_SOFTMAX <= THREADS * REGS_LAUNCH, "register split");
   static_assert(SMEM <= 232448 && COL_O + 2 * DHP <= 512, "budgets of one SM");
 };
@@ -63,8 +68,8 @@ struct SeqWork {
   int n_tree, ts;                 // tiles of new rows; tokens per slot
   bool same;
   int lo0, hi0;                   // slot 0 (slot 1 takes all of t0 .. t1)
-  __device__ __forceinline__ SeqWork(const SeqParams& p, int idx) {
-    const int4* src = reinterpret_cast<const int4*>(p.items + idx);
+  __device__ __forceinline__ SeqWork(const SeqParams& p, int work) {
+    const int4* src = reinterpret_cast<const int4*>(p.items + work / p.Hkv);
     const int4 x = src[0], y = src[1];
     it.row0 = x.x; it.rows = x.y; it.a = x.z; it.b = x.w; it.c = y.x; it.t0 = y.y; it.t1 = y.z; it.part = y.w;
     n_tree = TREE ? seq_tree_tiles(p, it) : 0;
@@ -80,6 +85,9 @@ struct SeqWork {
     }
   }
   __device__ __forceinline__ bool takes(int s, int t) const { return same ? ((t - it.t0) & 1) == s : s == 1 || (t >= lo0 && t < hi0); }
+  // the same as a range: first tile of slot s, end, step
+  __device__ __forceinline__ int first(int s) const { return same ? it.t0 + s : s == 0 ? lo0 : it.t0; }
+  __device__ __forceinline__ int end(int s) const { return same || s == 1 ? it.t1 : hi0; }
   __device__ __forceinline__ int first_token(int s) const { return same ? 0 : s * ts; }
   __device__ __forceinline__ int tokens(int s) const { return same ? it.rows : s == 0 ? ts : it.rows - ts; }
   // whether a row of the item does not see all keys of the tile
@@ -87,8 +95,6 @@ struct SeqWork {
   // whether the value tile is mended: see the top
   __device__ __forceinline__ bool mended(const SeqTile& k, bool again) const { return again ? masked(k) : TREE && k.kind == 1 && k.j0 + 128 > k.n; }
 };
-
-__device__ __forceinline__ bool not_finite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
 // Adds to a[0..31] (columns c0.. of a row's result) the values that are not finite of the keys that the row sees in masked tiles.
 template <bool TREE>
@@ -121,13 +127,30 @@ __device__ __noinline__ void seq_add_not_finite(const SeqParams& p, const SeqWor
   }
 }
 
+// The items of a CTA, one after the other; in the second pass the ones whose result was not finite (a bit each in `bad`).
+struct SeqWalk {
+  int k, work;                      // items seen; the current (item, head of keys), -1: the end
+  __device__ __forceinline__ void next(const SeqParams& p, const uint32_t* bad, bool again) {
+    const int n_work = p.plan->n_items * p.Hkv;
+    for (;;) {
+      const int64_t first = (int64_t)k * gridDim.x;
+      if (first >= n_work) { work = -1; return; }
+      work = (int)first + ((k & 1) ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x);
+      const int bit = min(k, 4095);
+      ++k;
+      if (work < n_work && (!again || ((bad[bit >> 5] >> (bit & 31)) & 1u))) break;
+    }
+  }
+  __device__ __forceinline__ SeqWalk(const SeqParams& p, const uint32_t* bad, bool again) : k(0) { next(p, bad, again); }
+};
+
 template <int DHP, bool TREE>
 __global__ void __launch_bounds__(384, 1)
 k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
               const __grid_constant__ CUtensorMap tmCK, const __grid_constant__ CUtensorMap tmCV, const __grid_constant__ SeqParams p) {
   using namespace tc;
   using C = SeqTcCfg<DHP>;
-  constexpr int STAGES = C::STAGES;
+  constexpr int STAGES = C::STAGES, QBUFS = C::QBUFS;
   extern __shared__ __align__(1024) uint8_t smem[];
   if ((smem_u32(smem) & 1023u) != 0) {                     // the swizzled tiles need a 1024-byte aligned base
     pdl_wait();
@@ -137,27 +160,34 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
   uint64_t* kv_full = bars;            // [10] keys or values of a tile landed
   uint64_t* kv_empty = bars + 10;      // [10] every MMA that reads them has run
-  uint64_t* q_full = bars + 20;
-  uint64_t* s_full = bars + 21;        // [2]  scores of the slot in TMEM
-  uint64_t* s_free = bars + 23;        // [2]  the values of the slot's last probabilities are issued: new scores may follow in the pipe
-  uint64_t* p_ready = bars + 25;       // [2]  probabilities in TMEM (four warps)
-  uint64_t* pv_done = bars + 27;       // [2]  the slot's accumulator is up to date
-  uint64_t* mend_done = bars + 29;     // [10] the value tile in this stage is mended
-  int* s_next = reinterpret_cast<int*>(bars + 39);          // [2 parities]
-  int* s_flags = s_next + 2;           // [3] of a pass: 1 a result is not finite, 2 a wait gave up, 4 values were taken out
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_flags + 3);
-  float* s_ml = reinterpret_cast<float*>(smem + C::OFF_ML);   // [2 slots][2][128]
+  uint64_t* mend_done = bars + 20;     // [10] the value tile in this stage is mended
+  uint64_t* q_full = bars + 30;        // [2]  queries of an item landed
+  uint64_t* q_empty = bars + 32;       // [2]  every score MMA that reads them has run
+  uint64_t* s_full = bars + 34;        // [2]  scores of the slot in TMEM
+  uint64_t* s_free = bars + 36;        // [2]  the values of the slot's last probabilities are issued: new scores may follow in the pipe
+  uint64_t* p_ready = bars + 38;       // [2]  probabilities in TMEM (four warps)
+  uint64_t* pv_done = bars + 40;       // [2]  the slot's accumulator is up to date
+  uint64_t* o_free = bars + 42;        // [2]  the slot's accumulator is read out, by its own warps (every item)
+  uint64_t* x_free = bars + 44;        // [2]  and by the other slot's (items whose slots are joined)
+  uint64_t* ml_full = bars + 46;       // [2]  the slot's references and sums are in shared memory (items whose slots are joined)
+  int* s_flags = reinterpret_cast<int*>(bars + 48);         // 1: some result is not finite, 2: a wait gave up
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_flags + 1);
+  float2* s_ml = reinterpret_cast<float2*>(smem + C::OFF_ML);
+  uint32_t* s_bad = reinterpret_cast<uint32_t*>(smem + C::OFF_BAD);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(&kv_full[i], 1); mbar_init(&kv_empty[i], 1); mbar_init(&mend_done[i], 1); }
-    mbar_init(q_full, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&s_free[i], 1); mbar_init(&p_ready[i], 4); mbar_init(&pv_done[i], 1); }
-    s_flags[0] = s_flags[1] = s_flags[2] = 0;
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&s_free[i], 1); mbar_init(&pv_done[i], 1);
+      mbar_init(&p_ready[i], 4); mbar_init(&o_free[i], 4); mbar_init(&x_free[i], 4); mbar_init(&ml_full[i], 4);
+    }
+    *s_flags = 0;
     fence_barrier_init();
     prefetch_tmap(&tmQ); prefetch_tmap(&tmK); prefetch_tmap(&tmV);
     if (TREE) { prefetch_tmap(&tmCK); prefetch_tmap(&tmCV); }
   }
+  if (threadIdx.x >= 128 && threadIdx.x < 256) s_bad[threadIdx.x - 128] = 0;
   if (warp == 1) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
@@ -166,30 +196,36 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   pdl_launch_dependents();
   pdl_wait();
 
-  const int n_work = p.plan->n_items * p.Hkv, G = p.G;
+  const int G = p.G;
   const int ksteps = (p.dh + 15) / 16;                      // of 16 features
-  int work = (int)blockIdx.x, turn = 0, pass_no = 0;        // an item and head of keys; how many this CTA has taken; passes over items
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_CONTROL));
     const uint32_t tmem_u = __shfl_sync(0xffffffffu, tmem_base, 0);
-    int g = 0;                                               // K and V tiles seen so far (ring position)
-    uint32_t ph0 = 0, ph1 = 0;                               // phase of the slot's barrier that this role waits for
-    uint32_t q_ph = 0, mend_ph = 0;                          // mend_ph: a bit for every stage
-    for (; work < n_work; ++turn) {
-      const int kvh = work % p.Hkv;
-      const SeqWork<TREE> w(p, work / p.Hkv);
-      for (int pass = 0;; ++pass, ++pass_no) {
-        const bool again = pass > 0;
-        bool ok = true;
+    bool ok = true;
+    int g = 0, qn = 0;                                       // tiles of keys and values so far (ring position); items with key tiles
+    uint32_t ph0 = 0, ph1 = 0;                               // phases of the slots' barriers that this role waits for
+    uint32_t mend_ph = 0;                                    // a bit for every stage
+    bool prev = false, prev_same = false;                    // an item before this one, and its slots were joined
+    uint32_t o_ph = 0, x_ph = 0;                             // phases in which that item's accumulators are read out
+    for (int pass = 0; pass < 2; ++pass) {
+      const bool again = pass > 0;
+      for (SeqWalk at(p, s_bad, again); ok && at.work >= 0; at.next(p, s_bad, again)) {
+        const int kvh = at.work % p.Hkv;
+        const SeqWork<TREE> w(p, at.work);
+        const bool any = w.it.t0 < w.it.t1;
+        const int qb = qn % QBUFS;
+        const uint32_t q_ph = (uint32_t)(qn / QBUFS) & 1u;
+        if (any) ++qn;
         if (warp == 0) {
           // ---------------------------------------------------------------- loads
-          if (!again && w.it.t0 < w.it.t1) {
+          if (any) {
+            if (!__all_sync(0xffffffffu, mbar_wait(&q_empty[qb], q_ph ^ 1u, p.err, 123))) { ok = false; break; }
             if (lane == 0) {
-              mbar_arrive_expect_tx(q_full, (w.same ? 1u : 2u) * (uint32_t)(w.ts * G) * 128u * (DHP / 64));
+              mbar_arrive_expect_tx(&q_full[qb], (w.same ? 1u : 2u) * (uint32_t)(w.ts * G) * 128u * (DHP / 64));
               for (int s = 0; s < (w.same ? 1 : 2); ++s)
                 for (int c = 0; c < DHP / 64; ++c)
-                  tma_load_3d(smem + C::OFF_Q + s * C::TILE + c * C::SUB, &tmQ, c * 64, kvh * G, w.it.row0 + s * w.ts, q_full);
+                  tma_load_3d(smem + C::OFF_Q + (qb * 2 + s) * C::TILE + c * C::SUB, &tmQ, c * 64, kvh * G, w.it.row0 + s * w.ts, &q_full[qb]);
             }
             __syncwarp();
           }
@@ -230,11 +266,8 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         } else if (warp == 1) {
           // ---------------------------------------------------------------- scores
           const uint32_t idesc = make_idesc_bf16(128, 128);
-          const uint64_t dq0 = make_sdesc_k_sw128(smem_u32(smem) + C::OFF_Q), dk0 = make_sdesc_k_sw128(smem_u32(smem) + C::OFF_KV);
-          if (!again && w.it.t0 < w.it.t1) {
-            ok = __all_sync(0xffffffffu, mbar_wait(q_full, q_ph, p.err, 112));
-            q_ph ^= 1u;
-          }
+          const uint64_t dq0 = make_sdesc_k_sw128(smem_u32(smem) + C::OFF_Q + qb * 2 * C::TILE), dk0 = make_sdesc_k_sw128(smem_u32(smem) + C::OFF_KV);
+          if (any && !__all_sync(0xffffffffu, mbar_wait(&q_full[qb], q_ph, p.err, 112))) { ok = false; break; }
           for (int t = w.it.t0; t < w.it.t1 && ok; ++t, g += 2) {
             const int st = g % STAGES;
             if (!__all_sync(0xffffffffu, mbar_wait(&kv_full[st], (uint32_t)(g / STAGES) & 1u, p.err, 113))) { ok = false; break; }
@@ -248,14 +281,17 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               const uint64_t dq = dq0 + (uint64_t)(w.same ? 0u : (uint32_t)s * C::TILE >> 4);
               if (elect_one()) {
                 for (int kk = 0; kk < ksteps; ++kk) {
-                  const uint64_t at = (uint64_t)(((kk >> 2) * C::SUB + (kk & 3) * 32) >> 4);
-                  mma_bf16_ss(tmem_u + C::COL_S + (uint32_t)s * 128, dq + at, dk + at, idesc, kk != 0);
+                  const uint64_t at_k = (uint64_t)(((kk >> 2) * C::SUB + (kk & 3) * 32) >> 4);
+                  mma_bf16_ss(tmem_u + C::COL_S + (uint32_t)s * 128, dq + at_k, dk + at_k, idesc, kk != 0);
                 }
                 mma_commit(&s_full[s]);
               }
               __syncwarp();
             }
-            if (ok && elect_one()) mma_commit(&kv_empty[st]);
+            if (ok && elect_one()) {
+              mma_commit(&kv_empty[st]);
+              if (t + 1 == w.it.t1) mma_commit(&q_empty[qb]);
+            }
             __syncwarp();
           }
         } else if (warp == 2) {
@@ -263,6 +299,10 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           const uint32_t idesc = make_idesc_bf16(128, ksteps * 16, false, true);
           const uint64_t dv0 = make_sdesc_mn_sw128(smem_u32(smem) + C::OFF_KV, C::SUB);
           bool first0 = true, first1 = true;
+          // the accumulator of slot s as the item before left it is read out
+          auto taken = [&](int s) {
+            return !prev || __all_sync(0xffffffffu, mbar_wait(&o_free[s], o_ph, p.err, 124) && (!prev_same || mbar_wait(&x_free[s], x_ph, p.err, 125)));
+          };
           for (int t = w.it.t0; t < w.it.t1 && ok; ++t, g += 2) {
             const int st = (g + 1) % STAGES;
             const SeqTile k = seq_tile<TREE>(p, w.it, w.n_tree, t);
@@ -276,6 +316,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               if (!w.takes(s, t)) continue;
               uint32_t& ph = s == 0 ? ph0 : ph1;
               bool& first = s == 0 ? first0 : first1;
+              if (first && !taken(s)) { ok = false; break; }
               if (!__all_sync(0xffffffffu, mbar_wait(&p_ready[s], ph, p.err, 117))) { ok = false; break; }
               ph ^= 1u;
               tc_fence_after();
@@ -294,17 +335,17 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             if (ok && elect_one()) mma_commit(&kv_empty[st]);
             __syncwarp();
           }
+          // every phase of these barriers is waited for, so that none is taken for the one two before it
+          if (ok && ((first0 && !taken(0)) || (first1 && !taken(1)))) ok = false;
+          if (prev) { o_ph ^= 1u; if (prev_same) x_ph ^= 1u; }
+          prev = true;
+          prev_same = w.same;
         } else {
-          // ---------------------------------------------------------------- items and mended value tiles
-          if (lane == 0) {
-            s_flags[(pass_no + 1) % 3] = 0;                  // nobody reads or sets it before the next pass
-            if (!again) s_next[turn & 1] = atomicAdd(&p.plan->taken, 1) + (int)gridDim.x;
-          }
-          // Every load of the item is waited for, so that a stage's phase is never taken for the one two before it; not at all where
-          // nothing is mended (a cached range ends in the last tile).
-          const bool any = w.it.t0 < w.it.t1 && (again || w.mended(seq_tile<TREE>(p, w.it, w.n_tree, w.it.t1 - 1), false));
+          // ---------------------------------------------------------------- value tiles that need mending
+          // Every load is waited for, so that a stage's phase is never taken for the one two before it (without a cache nothing is mended
+          // in the first pass, and all of its loads have landed before the second).
           for (int t = w.it.t0; t < w.it.t1 && ok; ++t, g += 2) {
-            if (!any) continue;
+            if (!TREE && !again) continue;
             const SeqTile k = seq_tile<TREE>(p, w.it, w.n_tree, t);
             const int st = (g + 1) % STAGES;
             if (!__all_sync(0xffffffffu, mbar_wait(&kv_full[g % STAGES], (uint32_t)(g / STAGES) & 1u, p.err, 119) &&
@@ -312,45 +353,37 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             if (!w.mended(k, again)) continue;
             uint8_t* tile = smem + C::OFF_KV + st * C::TILE;
             const int n = k.n - k.j0;                        // rows of the tile that there are
-            bool out = false;
             for (int i = lane; i < 128 * (DHP / 64) * 8; i += 32) {
               const int r = (i >> 3) & 127;
               if (r < n && !again) continue;
-              uint4* at = reinterpret_cast<uint4*>(tile + (i >> 10) * C::SUB + (i & 1023) * 16);
+              uint4* piece = reinterpret_cast<uint4*>(tile + (i >> 10) * C::SUB + (i & 1023) * 16);
               uint4 x = make_uint4(0, 0, 0, 0);
               if (r < n) {
-                x = *at;
+                x = *piece;
                 uint32_t* u = reinterpret_cast<uint32_t*>(&x);
-                bool any = false;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (not_finite2(u[e])) {
-                    any = true;
-                    if ((u[e] & 0x7f80u) == 0x7f80u) u[e] &= 0xffff0000u;
-                    if ((u[e] & 0x7f800000u) == 0x7f800000u) u[e] &= 0xffffu;
-                  }
-                if (!any) continue;
-                out = true;
+                for (int e = 0; e < 4; ++e) {
+                  if ((u[e] & 0x7f80u) == 0x7f80u) u[e] &= 0xffff0000u;
+                  if ((u[e] & 0x7f800000u) == 0x7f800000u) u[e] &= 0xffffu;
+                }
               }
-              *at = x;
+              *piece = x;
             }
-            if (out) atomicOr(&s_flags[pass_no % 3], 4);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&mend_done[st]);
           }
         }
-        if (!ok && lane == 0) atomicOr(&s_flags[pass_no % 3], 2);
-        __syncthreads();
-        const int flags = s_flags[pass_no % 3];
-        if ((flags & 2) && warp == 0) {
-          // giving up: let the copies already issued land (bounded) before this CTA's shared memory goes away
-          for (int j = 0; j < g && j < STAGES; ++j) mbar_wait_quiet(&kv_full[(g - 1 - j) % STAGES], (uint32_t)((g - 1 - j) / STAGES) & 1u);
-        }
-        __syncthreads();
-        if (flags & 2) { work = n_work; break; }
-        if (!(flags & 1) || again) { work = s_next[turn & 1]; ++pass_no; break; }
       }
+      if (!ok && lane == 0) atomicOr(s_flags, 2);
+      __syncthreads();
+      const int flags = *s_flags;
+      if ((flags & 2) && warp == 0) {
+        // giving up: let the copies already issued land (bounded) before this CTA's shared memory goes away
+        for (int j = 0; j < g && j < STAGES; ++j) mbar_wait_quiet(&kv_full[(g - 1 - j) % STAGES], (uint32_t)((g - 1 - j) / STAGES) & 1u);
+        for (int j = 0; j < qn && j < QBUFS; ++j) mbar_wait_quiet(&q_full[(qn - 1 - j) % QBUFS], (uint32_t)((qn - 1 - j) / QBUFS) & 1u);
+      }
+      if (flags != 1) break;
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::REGS_SOFTMAX));
@@ -359,22 +392,43 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     const int r = q * 32 + lane;                             // stacked row
     const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16);
     const uint32_t s_addr = lane_addr + C::COL_S + (uint32_t)s * 128, o_addr = lane_addr + C::COL_O + (uint32_t)(s * DHP);
+    const uint32_t other = lane_addr + C::COL_O + (uint32_t)((s ^ 1) * DHP);
     const float scale = p.scale_log2;
-    uint32_t s_ph = 0, pv_ph = 0;                            // pv_ph: of the slot's next value contraction
-    for (; work < n_work; ++turn) {
-      const int kvh = work % p.Hkv;
-      const SeqWork<TREE> w(p, work / p.Hkv);
-      const int rows = w.tokens(s) * G, tok = w.first_token(s) + min(r, max(rows - 1, 0)) / G;
-      const bool valid = r < rows, any_valid = q * 32 < rows;
-      bool mine = false;                                     // the slot took a tile: its accumulator holds something
-      for (int pass = 0;; ++pass, ++pass_no) {
-        bool ok = true;
+    // 4 x 4 transpose of 16-byte pieces inside each group of four lanes: lane 4j + i then holds piece i of rows 4j .. 4j + 3, so that
+    // every store instruction writes whole 64-byte parts of rows
+    auto xchg = [&](uint4& keep_lo, uint4& keep_hi, bool upper, int dist) {
+      // lanes with `upper` clear give away keep_hi and receive into it; lanes with it set give away keep_lo
+      uint4 send = upper ? keep_lo : keep_hi, recv;
+      recv.x = __shfl_xor_sync(0xffffffffu, send.x, dist); recv.y = __shfl_xor_sync(0xffffffffu, send.y, dist);
+      recv.z = __shfl_xor_sync(0xffffffffu, send.z, dist); recv.w = __shfl_xor_sync(0xffffffffu, send.w, dist);
+      if (upper) keep_lo = recv; else keep_hi = recv;
+    };
+    auto transpose4 = [&](uint4 (&t)[4]) {
+      xchg(t[0], t[1], (lane & 1) != 0, 1);
+      xchg(t[2], t[3], (lane & 1) != 0, 1);
+      xchg(t[0], t[2], (lane & 2) != 0, 2);
+      xchg(t[1], t[3], (lane & 2) != 0, 2);
+    };
+    bool ok = true;
+    uint32_t s_ph = 0, pv_ph = 0, joined = 0;                // pv_ph: of the slot's next value contraction; joined: items with joined slots
+    for (int pass = 0; pass < 2; ++pass) {
+      for (SeqWalk at(p, s_bad, pass > 0); ok && at.work >= 0; at.next(p, s_bad, pass > 0)) {
+        bool valid, any_valid, mine = false;                 // mine: the slot took a tile, its accumulator holds something
         float m = -INFINITY, l = 0.f;
-        int anc = w.it.c + tok;
-        mine = false;
-        for (int t = w.it.t0; t < w.it.t1; ++t) {
-          if (!w.takes(s, t)) continue;
-          const SeqTile k = seq_tile<TREE>(p, w.it, w.n_tree, t);
+        // What the tile loop needs of the item, in few registers (a tile's scores take 128); the rest is read again behind it.
+        int t, end, step, n_tree, vis, anc, first_row, first_top = 0;       // vis: keys (history) or cached rows (tree) that the row sees
+        {
+          const SeqWork<TREE> w(p, at.work);
+          const int rows = w.tokens(s) * G, tok = w.first_token(s) + min(r, max(rows - 1, 0)) / G;
+          valid = r < rows; any_valid = q * 32 < rows;
+          t = w.first(s); end = w.end(s); step = w.same ? 2 : 1;
+          n_tree = TREE ? w.n_tree : 0;
+          vis = TREE ? w.it.b : w.it.c + tok;
+          anc = w.it.c + tok;
+          first_row = w.it.row0 - w.it.c;
+          if (TREE) { const int top = ((w.it.c + w.it.rows + 127) >> 7) - 1; first_top = top; }
+        }
+        for (; t < end; t += step) {
           if (!__all_sync(0xffffffffu, mbar_wait(&s_full[s], s_ph, p.err, 120))) { ok = false; break; }
           s_ph ^= 1u;
           if (any_valid) {
@@ -383,20 +437,21 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 #pragma unroll
             for (int c = 0; c < 128; c += 32) tmem_ld_32x32(s_addr + c, *reinterpret_cast<float(*)[32]>(&v[c]));
             tmem_wait_ld();
-            if (TREE && k.kind == 2) {
+            if (TREE && t < n_tree) {
+              const int j0 = (first_top - t) * 128;
               uint32_t see[4] = {0u, 0u, 0u, 0u};
-              while (anc >= k.j0 + 128) anc = seq_parent(p, w.it.row0 - w.it.c, anc);
-              while (anc >= k.j0) {
-                const int b = anc - k.j0;
+              while (anc >= j0 + 128) anc = seq_parent(p, first_row, anc);
+              while (anc >= j0) {
+                const int b = anc - j0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) see[i] |= (b >> 5) == i ? 1u << (b & 31) : 0u;
-                anc = seq_parent(p, w.it.row0 - w.it.c, anc);
+                anc = seq_parent(p, first_row, anc);
               }
 #pragma unroll
               for (int j = 0; j < 128; ++j)
                 if (((see[j >> 5] >> (j & 31)) & 1u) == 0) v[j] = -INFINITY;
             } else {
-              const int n = (k.kind == 0 ? w.it.c + tok : k.n) - k.j0;           // keys of the tile that the row sees
+              const int n = vis - (t - n_tree) * 128;                            // keys of the tile that the row sees
               if (__any_sync(0xffffffffu, n < 128)) {
 #pragma unroll
                 for (int j = 0; j < 128; ++j)
@@ -453,54 +508,46 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           pv_ph ^= 1u;
           mine = true;
         }
-        // the slot's result complete?  any of it not finite?
-        bool bad = false;
-        if (mine && ok) {
-          ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[s], pv_ph ^ 1u, p.err, 122));
-          tc_fence_after();
-          if (ok && any_valid && pass == 0) {
-            float z = 0.f;
-#pragma unroll 1
-            for (int c = 0; c < ksteps * 16; c += 16) {
-              float a[16];
-              tmem_ld_32x16(o_addr + c, a);
-              tmem_wait_ld();
-#pragma unroll
-              for (int j = 0; j < 16; ++j) z = fmaf(a[j], 0.f, z);
-            }
-            bad = valid && z != 0.f;                         // 0 * infinity and 0 * NaN
-          }
+        if (!ok) break;
+        const SeqWork<TREE> w(p, at.work);
+        const int kvh = at.work % p.Hkv, tok = w.first_token(s) + min(r, max(w.tokens(s) * G - 1, 0)) / G;
+        if (mine && !__all_sync(0xffffffffu, mbar_wait(&pv_done[s], pv_ph ^ 1u, p.err, 122))) { ok = false; break; }
+        // ------------------------------------------------------------------ result: the slot's rows, or of joined slots half the columns
+        float w0 = 1.f, w1 = 0.f;                            // of this slot's accumulator and the other's
+        const bool have0 = mine, have1 = w.same && w.it.t1 - w.it.t0 > (s ^ 1);
+        if (w.same) {
+          // (read for the joined item before this one: its value contractions were behind that, but this slot may have had no tile)
+          if (joined > 0 && !__all_sync(0xffffffffu, mbar_wait(&x_free[s], (joined - 1) & 1u, p.err, 127))) { ok = false; break; }
+          s_ml[s * 128 + r] = make_float2(m, mine ? l : 0.f);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ml_full[s]);
+          if (!__all_sync(0xffffffffu, mbar_wait(&ml_full[s ^ 1], joined & 1u, p.err, 126))) { ok = false; break; }
+          ++joined;
+          const float2 o = s_ml[(s ^ 1) * 128 + r];
+          const float mm = fmaxf(m, o.x), ref = mm == -INFINITY ? 0.f : mm;
+          w0 = seq_ex2((m - ref) * scale); w1 = seq_ex2((o.x - ref) * scale);
+          l = l * w0 + o.y * w1;
+          m = mm;
         }
-        if (w.same) { s_ml[s * 256 + r] = m; s_ml[s * 256 + 128 + r] = mine ? l : 0.f; }
-        if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(&s_flags[pass_no % 3], 1);
-        if (!ok && lane == 0) atomicOr(&s_flags[pass_no % 3], 2);
-        tc_fence_before();
-        __syncthreads();
         tc_fence_after();
-        const int flags = s_flags[pass_no % 3];
-        const bool last = !(flags & 1) || pass > 0;
-        if (last && !(flags & 2) && any_valid) {
-          // ---------------------------------------------------------------- result: the slot's rows, or the half of the columns of both's
-          float w0 = 1.f, w1 = 0.f;                          // of this slot's accumulator and the other's
-          bool have0 = mine, have1 = false;
-          if (w.same) {
-            const float mo = s_ml[(s ^ 1) * 256 + r], lo = s_ml[(s ^ 1) * 256 + 128 + r], mm = fmaxf(m, mo);
-            const float ref = mm == -INFINITY ? 0.f : mm;
-            have1 = w.it.t1 - w.it.t0 > (s ^ 1);
-            w0 = seq_ex2((m - ref) * scale); w1 = seq_ex2((mo - ref) * scale);
-            l = l * w0 + lo * w1;
-            m = mm;
-          }
-          const int c_lo = w.same ? s * (DHP / 2) : 0, c_hi = w.same ? c_lo + DHP / 2 : DHP;
-          const uint32_t other = lane_addr + C::COL_O + (uint32_t)((s ^ 1) * DHP);
+        if (any_valid) {
+          const int c_lo = w.same ? s * (DHP / 2) : 0, c_hi = min(w.same ? c_lo + DHP / 2 : DHP, p.dh);
+          const bool whole = w.it.part < 0;
           const int64_t part = (int64_t)w.it.part * p.Hkv + kvh;
           const int R = p.tok * G, pr = w.first_token(s) * G + r;
-          if (w.it.part >= 0 && valid && (s == 0 || !w.same)) {
+          if (!whole && valid && (s == 0 || !w.same)) {
             p.part_ml[part * 2 * R + pr] = m == -INFINITY ? m : m * scale;
             p.part_ml[(part * 2 + 1) * R + pr] = l;
           }
-          const float inv = w.it.part >= 0 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-          uint8_t* stage = smem + C::OFF_Q + s * C::TILE + q * (C::TILE / 4);    // this warp's rows (the queries are done with)
+          const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+          w0 *= inv; w1 *= inv;
+          // where this row goes (element offset in the output, or in the partial results); -1: nowhere
+          const int64_t to = !valid ? -1 : whole ? (int64_t)(w.it.row0 + tok) * p.out_stride + (kvh * G + r % G) * p.dh : (part * R + pr) * p.dh;
+          int64_t to4[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) to4[i] = __shfl_sync(0xffffffffu, to, (lane & ~3) + i);
+          float z = 0.f;
 #pragma unroll 1
           for (int c = c_lo; c < c_hi; c += 32) {
             float a[32];
@@ -517,42 +564,55 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 #pragma unroll
               for (int j = 0; j < 32; ++j) a[j] = fmaf(b[j], w1, a[j]);
             }
-            if ((flags & 4) && valid) seq_add_not_finite<TREE>(p, w, tok, kvh, w.same || s == 1 ? w.it.t0 : w.lo0, w.same || s == 1 ? w.it.t1 : w.hi0, c, a);
-            __syncwarp();
-            if (w.it.part >= 0) {
-              if (valid) {
-                float* dst = p.part_acc + (part * R + pr) * p.dh + c;
-#pragma unroll
-                for (int j = 0; j < 32; j += 4)
-                  if (c + j < p.dh) *reinterpret_cast<float4*>(dst + j) = make_float4(a[j], a[j + 1], a[j + 2], a[j + 3]);
-              }
+            if (pass > 0) {
+              if (valid) seq_add_not_finite<TREE>(p, w, tok, kvh, w.same || s == 1 ? w.it.t0 : w.lo0, w.same || s == 1 ? w.it.t1 : w.hi0, c, a);
+              __syncwarp();
             } else {
 #pragma unroll
-              for (int j = 0; j < 32; j += 8)
-                *reinterpret_cast<uint4*>(stage + lane * (DHP * 2) + ((((c - c_lo + j) >> 3) ^ (lane & 7)) << 4)) =
-                    make_uint4(seq_pack(a[j] * inv, a[j + 1] * inv), seq_pack(a[j + 2] * inv, a[j + 3] * inv), seq_pack(a[j + 4] * inv, a[j + 5] * inv),
-                               seq_pack(a[j + 6] * inv, a[j + 7] * inv));
+              for (int j = 0; j < 32; ++j)
+                if (c + (j & ~7) < p.dh) z = fmaf(a[j], 0.f, z);               // 0 * infinity and 0 * NaN
             }
-          }
-          if (w.it.part < 0) {
-            __syncwarp();
-            const int chunks = (c_hi - c_lo) / 8, per = 32 / chunks;             // 16-byte pieces of a row; rows a store covers
-            for (int i = 0; i < 32; i += per) {
-              const int rr = i + lane / chunks, ch = lane % chunks, row = q * 32 + rr;
-              if (row < rows && c_lo + ch * 8 < p.dh) {
-                const uint4 x = *reinterpret_cast<const uint4*>(stage + rr * (DHP * 2) + ((ch ^ (rr & 7)) << 4));
-                const int token = w.first_token(s) + row / G;
-                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + (int64_t)(w.it.row0 + token) * p.out_stride + (kvh * G + row % G) * p.dh + c_lo + ch * 8) = x;
+            if (whole) {
+              uint4 t4[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                t4[i] = make_uint4(seq_pack(a[8 * i], a[8 * i + 1]), seq_pack(a[8 * i + 2], a[8 * i + 3]), seq_pack(a[8 * i + 4], a[8 * i + 5]), seq_pack(a[8 * i + 6], a[8 * i + 7]));
+              transpose4(t4);
+              const int col = c + (lane & 3) * 8;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (to4[i] >= 0 && col < p.dh) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + to4[i] + col) = t4[i];
+            } else {
+#pragma unroll
+              for (int h = 0; h < 32; h += 16) {
+                uint4 t4[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  t4[i] = make_uint4(__float_as_uint(a[h + 4 * i]), __float_as_uint(a[h + 4 * i + 1]), __float_as_uint(a[h + 4 * i + 2]), __float_as_uint(a[h + 4 * i + 3]));
+                transpose4(t4);
+                const int col = c + h + (lane & 3) * 4;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  if (to4[i] >= 0 && col < p.dh) *reinterpret_cast<uint4*>(p.part_acc + to4[i] + col) = t4[i];
               }
             }
+          }
+          if (__any_sync(0xffffffffu, valid && z != 0.f) && lane == 0) {
+            const int bit = min(at.k - 1, 4095);
+            atomicOr(&s_bad[bit >> 5], 1u << (bit & 31));
+            atomicOr(s_flags, 1);
           }
         }
         tc_fence_before();
-        fence_proxy_async_smem();                            // the next queries arrive by TMA where the rows were staged
-        __syncthreads();
-        if (flags & 2) { work = n_work; break; }
-        if (last) { work = s_next[turn & 1]; ++pass_no; break; }
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&o_free[s]);
+          if (w.same) mbar_arrive(&x_free[s ^ 1]);
+        }
       }
+      if (!ok && lane == 0) atomicOr(s_flags, 2);
+      __syncthreads();
+      if (*s_flags != 1) break;
     }
   }
 

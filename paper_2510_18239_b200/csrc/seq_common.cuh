@@ -23,7 +23,7 @@ struct SeqItem {
   int32_t part;           // where the partial result goes; -1: the item is the whole row tile
 };
 struct SeqSplit { int32_t row0, rows, part0, n; };       // a row tile cut into n items, parts part0 ..
-struct SeqPlan { int32_t n_items, n_split, n_parts, taken; };     // taken: items fetched beyond the first of every CTA
+struct SeqPlan { int32_t n_items, n_split, n_parts, pad; };
 
 struct SeqParams {
   const void *q, *k, *v;                 // history: k, v the packed keys; tree: the new rows' (nullable)
