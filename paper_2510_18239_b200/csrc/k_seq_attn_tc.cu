@@ -36,17 +36,25 @@ struct SeqTcCfg {
   static constexpr uint32_t OFF_ML = OFF_BAR + 512;               // references and sums of joined slots: [2 slots][128] pairs
   static constexpr uint32_t OFF_BAD = OFF_ML + 2 * 128 * 8;       // a bit for every item of the CTA
   static constexpr uint32_t SMEM = OFF_BAD + 512;
-  static constexpr uint32_t COL_S = 0, COL_O = 256;                // scores: two of 128 columns; accumulators: two of DHP
-  static constexpr int REGS_LAUNCH = 168, REGS_CONTROL = 56, REGS_SOFTMAX = 224;
+  // tensor memory: scores, two of 128 columns; accumulators, two of DHP; probabilities, two of 64: their own with DHP = 64, so that the next
+  // scores are formed while these are worked out; over the scores they come from with DHP = 128
+  static constexpr bool OWN_P = DHP == 64;
+  static constexpr uint32_t COL_S = 0, COL_P = OWN_P ? 256 : 0, P_STEP = OWN_P ? 64 : 128, COL_O = 512 - 2 * DHP;
+  static constexpr int REGS_LAUNCH = 168, REGS_CONTROL = 104, REGS_SOFTMAX = 200;
   static_assert(128 * REGS_CONTROL + 256 * REGS_SOFTMAX <= THREADS * REGS_LAUNCH, "register split");
-  static_assert(SMEM <= 232448 && COL_O + 2 * DHP <= 512, "budgets of one SM");
+  static_assert(SMEM <= 232448, "shared memory of one SM");
 };
-constexpr float kSeqRescale = 8.0f;                                // log2 units
+constexpr float kSeqRescale = 8.0f, kSeqBelow = 60.0f, kSeqAbove = 100.0f;        // log2 units
 constexpr int kRowNowhere = 0x7fff0000;                            // a row past the end of every tensor map: reads as zeros
 
 __device__ __forceinline__ float seq_ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float seq_max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
 __device__ __forceinline__ uint32_t seq_pack(float lo, float hi) {
@@ -164,13 +172,15 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   uint64_t* q_full = bars + 30;        // [2]  queries of an item landed
   uint64_t* q_empty = bars + 32;       // [2]  every score MMA that reads them has run
   uint64_t* s_full = bars + 34;        // [2]  scores of the slot in TMEM
-  uint64_t* s_free = bars + 36;        // [2]  the values of the slot's last probabilities are issued: new scores may follow in the pipe
+  uint64_t* s_free = bars + 36;        // [2]  new scores may be formed: the last are in registers (four warps; OWN_P), or the values of the
+                                       //      probabilities over them are issued, which the pipe then takes first
   uint64_t* p_ready = bars + 38;       // [2]  probabilities in TMEM (four warps)
   uint64_t* pv_done = bars + 40;       // [2]  the slot's accumulator is up to date
   uint64_t* o_free = bars + 42;        // [2]  the slot's accumulator is read out, by its own warps (every item)
   uint64_t* x_free = bars + 44;        // [2]  and by the other slot's (items whose slots are joined)
+  uint64_t* p_half = bars + 48;        // [2]  the first half of them
   uint64_t* ml_full = bars + 46;       // [2]  the slot's references and sums are in shared memory (items whose slots are joined)
-  int* s_flags = reinterpret_cast<int*>(bars + 48);         // 1: some result is not finite, 2: a wait gave up
+  int* s_flags = reinterpret_cast<int*>(bars + 50);         // 1: some result is not finite, 2: a wait gave up
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_flags + 1);
   float2* s_ml = reinterpret_cast<float2*>(smem + C::OFF_ML);
   uint32_t* s_bad = reinterpret_cast<uint32_t*>(smem + C::OFF_BAD);
@@ -179,8 +189,8 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(&kv_full[i], 1); mbar_init(&kv_empty[i], 1); mbar_init(&mend_done[i], 1); }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&s_free[i], 1); mbar_init(&pv_done[i], 1);
-      mbar_init(&p_ready[i], 4); mbar_init(&o_free[i], 4); mbar_init(&x_free[i], 4); mbar_init(&ml_full[i], 4);
+      mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&s_free[i], C::OWN_P ? 4 : 1); mbar_init(&pv_done[i], 1);
+      mbar_init(&p_ready[i], 4); mbar_init(&p_half[i], 4); mbar_init(&o_free[i], 4); mbar_init(&x_free[i], 4); mbar_init(&ml_full[i], 4);
     }
     *s_flags = 0;
     fence_barrier_init();
@@ -280,10 +290,11 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               tc_fence_after();
               const uint64_t dq = dq0 + (uint64_t)(w.same ? 0u : (uint32_t)s * C::TILE >> 4);
               if (elect_one()) {
-                for (int kk = 0; kk < ksteps; ++kk) {
-                  const uint64_t at_k = (uint64_t)(((kk >> 2) * C::SUB + (kk & 3) * 32) >> 4);
-                  mma_bf16_ss(tmem_u + C::COL_S + (uint32_t)s * 128, dq + at_k, dk + at_k, idesc, kk != 0);
-                }
+#pragma unroll
+                for (int kk = 0; kk < DHP / 16; ++kk)
+                  if (kk < ksteps)
+                    mma_bf16_ss(tmem_u + C::COL_S + (uint32_t)s * 128, dq + (((kk >> 2) * C::SUB + (kk & 3) * 32) >> 4),
+                                dk + (((kk >> 2) * C::SUB + (kk & 3) * 32) >> 4), idesc, kk != 0);
                 mma_commit(&s_full[s]);
               }
               __syncwarp();
@@ -317,17 +328,26 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               uint32_t& ph = s == 0 ? ph0 : ph1;
               bool& first = s == 0 ? first0 : first1;
               if (first && !taken(s)) { ok = false; break; }
+              auto half = [&](int k0) {
+#pragma unroll
+                for (int kk = k0; kk < k0 + 4; ++kk)
+                  mma_bf16_ts(tmem_u + C::COL_O + (uint32_t)(s * DHP), tmem_u + C::COL_P + (uint32_t)(s * C::P_STEP + kk * 8), dv + ((kk * 2048) >> 4), idesc,
+                              kk != 0 || !first ? 1u : 0u);
+              };
+              if (!__all_sync(0xffffffffu, mbar_wait(&p_half[s], ph, p.err, 128))) { ok = false; break; }
+              tc_fence_after();
+              if (elect_one()) half(0);
+              __syncwarp();
               if (!__all_sync(0xffffffffu, mbar_wait(&p_ready[s], ph, p.err, 117))) { ok = false; break; }
               ph ^= 1u;
               tc_fence_after();
               if (elect_one()) {
-#pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
-                  mma_bf16_ts(tmem_u + C::COL_O + (uint32_t)(s * DHP), tmem_u + C::COL_S + (uint32_t)(s * 128 + kk * 8), dv + ((kk * 2048) >> 4), idesc,
-                              kk != 0 || !first ? 1u : 0u);
+                half(4);
                 mma_commit(&pv_done[s]);
-                tc_fence_before();
-                mbar_arrive(&s_free[s]);
+                if (!C::OWN_P) {
+                  tc_fence_before();
+                  mbar_arrive(&s_free[s]);
+                }
               }
               first = false;
               __syncwarp();
@@ -392,6 +412,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     const int r = q * 32 + lane;                             // stacked row
     const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16);
     const uint32_t s_addr = lane_addr + C::COL_S + (uint32_t)s * 128, o_addr = lane_addr + C::COL_O + (uint32_t)(s * DHP);
+    const uint32_t p_addr = lane_addr + C::COL_P + (uint32_t)s * C::P_STEP;
     const uint32_t other = lane_addr + C::COL_O + (uint32_t)((s ^ 1) * DHP);
     const float scale = p.scale_log2;
     // 4 x 4 transpose of 16-byte pieces inside each group of four lanes: lane 4j + i then holds piece i of rows 4j .. 4j + 3, so that
@@ -409,12 +430,17 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       xchg(t[0], t[2], (lane & 2) != 0, 2);
       xchg(t[1], t[3], (lane & 2) != 0, 2);
     };
+    // scores with this maximum against reference m, or against 0 where there was none yet: 2^(score - m) leaves the range that bf16 and
+    // fp32 sums are safe in
+    auto too_far = [](float top, float m) { return m == -INFINITY ? top < -kSeqBelow || top > kSeqAbove : top > m + kSeqAbove; };
     bool ok = true;
     uint32_t s_ph = 0, pv_ph = 0, joined = 0;                // pv_ph: of the slot's next value contraction; joined: items with joined slots
     for (int pass = 0; pass < 2; ++pass) {
       for (SeqWalk at(p, s_bad, pass > 0); ok && at.work >= 0; at.next(p, s_bad, pass > 0)) {
         bool valid, any_valid, mine = false;                 // mine: the slot took a tile, its accumulator holds something
-        float m = -INFINITY, l = 0.f;
+        // m: reference of the row (log2 domain) in use, m_next: from the next tile on, l: sum so far
+        float m = -INFINITY, m_next = m, l = 0.f;
+        bool far = false;
         // What the tile loop needs of the item, in few registers (a tile's scores take 128); the rest is read again behind it.
         int t, end, step, n_tree, vis, anc, first_row, first_top = 0;       // vis: keys (history) or cached rows (tree) that the row sees
         {
@@ -433,13 +459,12 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           s_ph ^= 1u;
           if (any_valid) {
             tc_fence_after();
-            float v[128];
-#pragma unroll
-            for (int c = 0; c < 128; c += 32) tmem_ld_32x32(s_addr + c, *reinterpret_cast<float(*)[32]>(&v[c]));
-            tmem_wait_ld();
-            if (TREE && t < n_tree) {
+            const bool new_rows = TREE && t < n_tree;
+            const int n = vis - (t - n_tree) * 128;          // keys of the tile that the row sees
+            bool masked = __any_sync(0xffffffffu, n < 128);
+            uint32_t see[4] = {0u, 0u, 0u, 0u};
+            if (new_rows) {
               const int j0 = (first_top - t) * 128;
-              uint32_t see[4] = {0u, 0u, 0u, 0u};
               while (anc >= j0 + 128) anc = seq_parent(p, first_row, anc);
               while (anc >= j0) {
                 const int b = anc - j0;
@@ -447,30 +472,44 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 for (int i = 0; i < 4; ++i) see[i] |= (b >> 5) == i ? 1u << (b & 31) : 0u;
                 anc = seq_parent(p, first_row, anc);
               }
+              __syncwarp();
+            } else if (masked) {
 #pragma unroll
-              for (int j = 0; j < 128; ++j)
-                if (((see[j >> 5] >> (j & 31)) & 1u) == 0) v[j] = -INFINITY;
-            } else {
-              const int n = vis - (t - n_tree) * 128;                            // keys of the tile that the row sees
-              if (__any_sync(0xffffffffu, n < 128)) {
+              for (int i = 0; i < 4; ++i) { const int left = n - 32 * i; see[i] = left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u; }
+            }
+            masked |= new_rows;
+            auto mask32 = [&](float (&v)[32], uint32_t bits) {
+              if (masked) {
 #pragma unroll
-                for (int j = 0; j < 128; ++j)
-                  if (j >= n) v[j] = -INFINITY;
+                for (int j = 0; j < 32; ++j)
+                  if (((bits >> j) & 1u) == 0) v[j] = -INFINITY;
               }
-            }
-            float mx0 = v[0], mx1 = v[1], mx2 = v[2], mx3 = v[3];
+            };
+            auto most32 = [&](const float (&v)[32], float mx) {
+              float a = v[0], b = v[1];
 #pragma unroll
-            for (int j = 4; j < 128; j += 4) {
-              mx0 = fmaxf(mx0, v[j]); mx1 = fmaxf(mx1, v[j + 1]); mx2 = fmaxf(mx2, v[j + 2]); mx3 = fmaxf(mx3, v[j + 3]);
+              for (int j = 2; j < 30; j += 4) { a = seq_max3(a, v[j], v[j + 2]); b = seq_max3(b, v[j + 1], v[j + 3]); }
+              return seq_max3(fmaxf(mx, v[30]), fmaxf(a, v[31]), b);
+            };
+            if (pass > 0) {
+              // The second time the maximum is known first.  It is taken where the reference would be too far off, and only there: whatever
+              // the item is done again for, the other rows come out as they did.
+              float mx = -INFINITY;
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                float v[32];
+                tmem_ld_32x32(s_addr + 32 * c, v);
+                tmem_wait_ld();
+                mask32(v, see[c]);
+                mx = most32(v, mx);
+              }
+              if (mx != -INFINITY && too_far(mx * scale, m_next)) m_next = mx * scale;
             }
-            const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
-            // raise the reference only when it is exceeded by more than the threshold, or unset
-            const bool need = valid && (mx - m) * scale > kSeqRescale;
-            const float m_new = need ? mx : m;
-            const float factor = need && m != -INFINITY ? seq_ex2((m - m_new) * scale) : 1.f;
-            if (mine && __any_sync(0xffffffffu, need)) {
+            const bool raise = valid && m_next != m;
+            if (mine && __any_sync(0xffffffffu, raise)) {
               if (!__all_sync(0xffffffffu, mbar_wait(&pv_done[s], pv_ph ^ 1u, p.err, 121))) { ok = false; break; }
               tc_fence_after();
+              const float factor = raise && m != -INFINITY ? seq_ex2(m - m_next) : 1.f;
 #pragma unroll 1
               for (int c = 0; c < DHP; c += 32) {
                 float a[32];
@@ -480,29 +519,79 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 for (int j = 0; j < 32; ++j) a[j] *= factor;
                 tmem_st_32x32(o_addr + c, a);
               }
+              l *= factor;
             }
-            l *= factor;
-            m = m_new;
-            const float ref = m == -INFINITY ? 0.f : m * scale;
+            m = m_next;
+            const float ref = m == -INFINITY ? 0.f : m;
+            float mx = -INFINITY;
             float2 s0 = make_float2(0.f, 0.f), s1 = s0;
             const float2 sc2 = make_float2(scale, scale), rf2 = make_float2(-ref, -ref);
-#pragma unroll
-            for (int c = 0; c < 128; c += 32) {
+            // 32 keys of the tile: probabilities, their sum, the maximum
+            auto chunk = [&](float (&x)[32], uint32_t bits, uint32_t to, bool first) {
+              mask32(x, bits);
               float packed[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) {
-                float2 e = __ffma2_rn(make_float2(v[c + 2 * j], v[c + 2 * j + 1]), sc2, rf2);
+                float2 e = __ffma2_rn(make_float2(x[2 * j], x[2 * j + 1]), sc2, rf2);
                 e = make_float2(seq_ex2(e.x), seq_ex2(e.y));
                 if (j & 1) s1 = __fadd2_rn(s1, e); else s0 = __fadd2_rn(s0, e);
                 packed[j] = __uint_as_float(seq_pack(e.x, e.y));
               }
-              tmem_st_32x16(s_addr + (uint32_t)(c >> 1), packed);
+              mx = most32(x, mx);
+              if (C::OWN_P && first && mine) {               // the last probabilities are read
+                ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[s], pv_ph ^ 1u, p.err, 129));
+                tc_fence_after();
+              }
+              tmem_st_32x16(to, packed);
+            };
+            // Rolled up: unrolled over the tile, the code of the roles does not stay in the instruction caches (twice the time).
+            float x0[32], x1[32];
+            tmem_ld_32x32(s_addr, x0);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+              tmem_wait_ld();
+              tmem_ld_32x32(s_addr + 64 * h + 32, x1);
+              chunk(x0, h ? see[2] : see[0], p_addr + 32 * h, h == 0);
+              tmem_wait_ld();
+              if (h == 0) {
+                tmem_ld_32x32(s_addr + 64, x0);
+              } else if (C::OWN_P) {                         // all scores are in registers
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s_free[s]);
+                __syncwarp();                                // (the whole warp loads from and stores to tensor memory)
+              }
+              chunk(x1, h ? see[3] : see[1], p_addr + 32 * h + 16, false);
+              if (h == 0) {
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_half[s]);
+                __syncwarp();
+              }
             }
             s0 = __fadd2_rn(s0, s1);
             l += s0.x + s0.y;
+            // the reference of the next tile
+            const float top = mx * scale;
+            if (mx != -INFINITY) {
+              far |= too_far(top, m);
+              if (m == -INFINITY) {
+                m = 0.f;
+                m_next = fabsf(top) > kSeqRescale ? top : 0.f;
+              } else {
+                m_next = top > m + kSeqRescale ? top : m;
+              }
+            }
             tmem_wait_st();
             tc_fence_before();
+          } else {
+            // a warp without rows keeps step: with scores ahead of the probabilities it could else arrive for a tile too early
+            if (lane == 0 && C::OWN_P) mbar_arrive(&s_free[s]);
+            if (C::OWN_P && mine) ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[s], pv_ph ^ 1u, p.err, 130));
+            if (lane == 0) mbar_arrive(&p_half[s]);
           }
+          if (!ok) break;
           __syncwarp();
           if (lane == 0) mbar_arrive(&p_ready[s]);
           pv_ph ^= 1u;
@@ -526,7 +615,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           ++joined;
           const float2 o = s_ml[(s ^ 1) * 128 + r];
           const float mm = fmaxf(m, o.x), ref = mm == -INFINITY ? 0.f : mm;
-          w0 = seq_ex2((m - ref) * scale); w1 = seq_ex2((o.x - ref) * scale);
+          w0 = seq_ex2(m - ref); w1 = seq_ex2(o.x - ref);
           l = l * w0 + o.y * w1;
           m = mm;
         }
@@ -537,7 +626,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           const int64_t part = (int64_t)w.it.part * p.Hkv + kvh;
           const int R = p.tok * G, pr = w.first_token(s) * G + r;
           if (!whole && valid && (s == 0 || !w.same)) {
-            p.part_ml[part * 2 * R + pr] = m == -INFINITY ? m : m * scale;
+            p.part_ml[part * 2 * R + pr] = m;
             p.part_ml[(part * 2 + 1) * R + pr] = l;
           }
           const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
@@ -547,7 +636,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           int64_t to4[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) to4[i] = __shfl_sync(0xffffffffu, to, (lane & ~3) + i);
-          float z = 0.f;
+          float z = pass > 0 ? 0.f : far ? 1.f : l * 0.f;         // not 0: not finite, or too far from the reference
 #pragma unroll 1
           for (int c = c_lo; c < c_hi; c += 32) {
             float a[32];
