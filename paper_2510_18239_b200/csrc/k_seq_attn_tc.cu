@@ -22,8 +22,7 @@
 //  * Masked positions have p = 0, but 0 * NaN and 0 * infinity are NaN.  Value rows behind the end of a cached range, which may never have
 //    been written, are zeroed in shared memory.  Elsewhere such values are the exception: an item whose result has a NaN or an infinity is
 //    done again with what is not finite taken out of every tile that masks anything; the rows that do see it get it added at the end.
-#include "seq_common.cuh"
-#include "tc_common.cuh"
+#include "seq_tc.cuh"
 
 namespace lime {
 
@@ -36,38 +35,11 @@ struct SeqTcCfg {
   static constexpr uint32_t OFF_ML = OFF_BAR + 512;               // references and sums of joined slots: [2 slots][128] pairs
   static constexpr uint32_t OFF_BAD = OFF_ML + 2 * 128 * 8;       // a bit for every item of the CTA
   static constexpr uint32_t SMEM = OFF_BAD + 512;
-  // tensor memory: scores, two of 128 columns; accumulators, two of DHP; probabilities, two of 64: their own with DHP = 64, so that the next
-  // scores are formed while these are worked out; over the scores they come from with DHP = 128
-  static constexpr bool OWN_P = DHP == 64;
-  static constexpr uint32_t COL_S = 0, COL_P = OWN_P ? 256 : 0, P_STEP = OWN_P ? 64 : 128, COL_O = 512 - 2 * DHP;
-  static constexpr int REGS_LAUNCH = 168, REGS_CONTROL = 104, REGS_SOFTMAX = 200;
+  static constexpr uint32_t COL_S = 0, COL_O = 256;                // scores: two of 128 columns; accumulators: two of DHP
+  static constexpr int REGS_LAUNCH = 168, REGS_CONTROL = 56, REGS_SOFTMAX = 224;
   static_assert(128 * REGS_CONTROL + 256 * REGS_SOFTMAX <= THREADS * REGS_LAUNCH, "register split");
-  static_assert(SMEM <= 232448, "shared memory of one SM");
+  static_assert(SMEM <= 232448 && COL_O + 2 * DHP <= 512, "budgets of one SM");
 };
-constexpr float kSeqRescale = 8.0f, kSeqBelow = 60.0f, kSeqAbove = 100.0f;        // log2 units
-constexpr int kRowNowhere = 0x7fff0000;                            // a row past the end of every tensor map: reads as zeros
-
-__device__ __forceinline__ float seq_ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float seq_max3(float a, float b, float c) {
-  float y;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
-  return y;
-}
-__device__ __forceinline__ uint32_t seq_pack(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* m, int x, int y, int z, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-      ::"r"(tc::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(tc::smem_u32(bar)), "r"(x), "r"(y), "r"(z)
-      : "memory");
-}
-
 // An item as its warps see it: key tiles t0 .. t1 (the walk of seq_common.cuh), slot s takes those of [lo[s], hi[s]), or, where both
 // slots hold the same rows (`same`), every other one.
 template <bool TREE>
@@ -77,9 +49,7 @@ struct SeqWork {
   bool same;
   int lo0, hi0;                   // slot 0 (slot 1 takes all of t0 .. t1)
   __device__ __forceinline__ SeqWork(const SeqParams& p, int work) {
-    const int4* src = reinterpret_cast<const int4*>(p.items + work / p.Hkv);
-    const int4 x = src[0], y = src[1];
-    it.row0 = x.x; it.rows = x.y; it.a = x.z; it.b = x.w; it.c = y.x; it.t0 = y.y; it.t1 = y.z; it.part = y.w;
+    it = seq_item(p, work);
     n_tree = TREE ? seq_tree_tiles(p, it) : 0;
     ts = p.tok / 2;
     same = it.rows <= ts;
@@ -99,57 +69,9 @@ struct SeqWork {
   __device__ __forceinline__ int first_token(int s) const { return same ? 0 : s * ts; }
   __device__ __forceinline__ int tokens(int s) const { return same ? it.rows : s == 0 ? ts : it.rows - ts; }
   // whether a row of the item does not see all keys of the tile
-  __device__ __forceinline__ bool masked(const SeqTile& k) const { return k.kind == 2 || (k.kind == 0 ? k.j0 + 128 > it.c : k.j0 + 128 > k.n); }
+  __device__ __forceinline__ bool masked(const SeqTile& k) const { return seq_masked(it, k, 128); }
   // whether the value tile is mended: see the top
   __device__ __forceinline__ bool mended(const SeqTile& k, bool again) const { return again ? masked(k) : TREE && k.kind == 1 && k.j0 + 128 > k.n; }
-};
-
-// Adds to a[0..31] (columns c0.. of a row's result) the values that are not finite of the keys that the row sees in masked tiles.
-template <bool TREE>
-__device__ __noinline__ void seq_add_not_finite(const SeqParams& p, const SeqWork<TREE>& w, int token, int kvh, int lo, int hi, int c0, float (&a)[32]) {
-  const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v);
-  auto add = [&](const __nv_bfloat16* row) {
-    for (int c = 0; c < 32; ++c)
-      if (c0 + c < p.dh) {
-        const float x = __bfloat162float(row[c0 + c]);
-        if (!(fabsf(x) < INFINITY)) a[c] += x;
-      }
-  };
-  for (int t = lo; t < hi; ++t) {
-    const SeqTile k = seq_tile<TREE>(p, w.it, w.n_tree, t);
-    if (!w.masked(k)) continue;
-    if (TREE && k.kind == 2) {
-      for (int j = w.it.c + token; j >= k.j0; j = seq_parent(p, w.it.row0 - w.it.c, j))
-        if (j < k.j0 + 128) add(v + (int64_t)(w.it.row0 - w.it.c + j) * p.v_stride + kvh * p.dh);
-    } else {
-      const int end = min(k.j0 + 128, TREE ? k.n : w.it.c + token);
-      for (int j = k.j0; j < end; ++j) {
-        if (!TREE) {
-          add(v + (int64_t)(w.it.a + j) * p.v_stride + kvh * p.dh);
-        } else {
-          const int64_t pg = seq_page(p, w.it.a, j);
-          if (pg < p.n_pages) add(static_cast<const __nv_bfloat16*>(p.cv) + ((pg * p.page_rows + (j & (p.page_rows - 1))) * p.Hkv + kvh) * p.dh);
-        }
-      }
-    }
-  }
-}
-
-// The items of a CTA, one after the other; in the second pass the ones whose result was not finite (a bit each in `bad`).
-struct SeqWalk {
-  int k, work;                      // items seen; the current (item, head of keys), -1: the end
-  __device__ __forceinline__ void next(const SeqParams& p, const uint32_t* bad, bool again) {
-    const int n_work = p.plan->n_items * p.Hkv;
-    for (;;) {
-      const int64_t first = (int64_t)k * gridDim.x;
-      if (first >= n_work) { work = -1; return; }
-      work = (int)first + ((k & 1) ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x);
-      const int bit = min(k, 4095);
-      ++k;
-      if (work < n_work && (!again || ((bad[bit >> 5] >> (bit & 31)) & 1u))) break;
-    }
-  }
-  __device__ __forceinline__ SeqWalk(const SeqParams& p, const uint32_t* bad, bool again) : k(0) { next(p, bad, again); }
 };
 
 template <int DHP, bool TREE>
@@ -172,15 +94,13 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   uint64_t* q_full = bars + 30;        // [2]  queries of an item landed
   uint64_t* q_empty = bars + 32;       // [2]  every score MMA that reads them has run
   uint64_t* s_full = bars + 34;        // [2]  scores of the slot in TMEM
-  uint64_t* s_free = bars + 36;        // [2]  new scores may be formed: the last are in registers (four warps; OWN_P), or the values of the
-                                       //      probabilities over them are issued, which the pipe then takes first
+  uint64_t* s_free = bars + 36;        // [2]  the values of the slot's last probabilities are issued: new scores may follow in the pipe
   uint64_t* p_ready = bars + 38;       // [2]  probabilities in TMEM (four warps)
   uint64_t* pv_done = bars + 40;       // [2]  the slot's accumulator is up to date
   uint64_t* o_free = bars + 42;        // [2]  the slot's accumulator is read out, by its own warps (every item)
   uint64_t* x_free = bars + 44;        // [2]  and by the other slot's (items whose slots are joined)
-  uint64_t* p_half = bars + 48;        // [2]  the first half of them
   uint64_t* ml_full = bars + 46;       // [2]  the slot's references and sums are in shared memory (items whose slots are joined)
-  int* s_flags = reinterpret_cast<int*>(bars + 50);         // 1: some result is not finite, 2: a wait gave up
+  int* s_flags = reinterpret_cast<int*>(bars + 48);         // 1: some result is not finite, 2: a wait gave up
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_flags + 1);
   float2* s_ml = reinterpret_cast<float2*>(smem + C::OFF_ML);
   uint32_t* s_bad = reinterpret_cast<uint32_t*>(smem + C::OFF_BAD);
@@ -189,8 +109,8 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(&kv_full[i], 1); mbar_init(&kv_empty[i], 1); mbar_init(&mend_done[i], 1); }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&s_free[i], C::OWN_P ? 4 : 1); mbar_init(&pv_done[i], 1);
-      mbar_init(&p_ready[i], 4); mbar_init(&p_half[i], 4); mbar_init(&o_free[i], 4); mbar_init(&x_free[i], 4); mbar_init(&ml_full[i], 4);
+      mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&s_free[i], 1); mbar_init(&pv_done[i], 1);
+      mbar_init(&p_ready[i], 4); mbar_init(&o_free[i], 4); mbar_init(&x_free[i], 4); mbar_init(&ml_full[i], 4);
     }
     *s_flags = 0;
     fence_barrier_init();
@@ -290,11 +210,10 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               tc_fence_after();
               const uint64_t dq = dq0 + (uint64_t)(w.same ? 0u : (uint32_t)s * C::TILE >> 4);
               if (elect_one()) {
-#pragma unroll
-                for (int kk = 0; kk < DHP / 16; ++kk)
-                  if (kk < ksteps)
-                    mma_bf16_ss(tmem_u + C::COL_S + (uint32_t)s * 128, dq + (((kk >> 2) * C::SUB + (kk & 3) * 32) >> 4),
-                                dk + (((kk >> 2) * C::SUB + (kk & 3) * 32) >> 4), idesc, kk != 0);
+                for (int kk = 0; kk < ksteps; ++kk) {
+                  const uint64_t at_k = (uint64_t)(((kk >> 2) * C::SUB + (kk & 3) * 32) >> 4);
+                  mma_bf16_ss(tmem_u + C::COL_S + (uint32_t)s * 128, dq + at_k, dk + at_k, idesc, kk != 0);
+                }
                 mma_commit(&s_full[s]);
               }
               __syncwarp();
@@ -328,26 +247,17 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               uint32_t& ph = s == 0 ? ph0 : ph1;
               bool& first = s == 0 ? first0 : first1;
               if (first && !taken(s)) { ok = false; break; }
-              auto half = [&](int k0) {
-#pragma unroll
-                for (int kk = k0; kk < k0 + 4; ++kk)
-                  mma_bf16_ts(tmem_u + C::COL_O + (uint32_t)(s * DHP), tmem_u + C::COL_P + (uint32_t)(s * C::P_STEP + kk * 8), dv + ((kk * 2048) >> 4), idesc,
-                              kk != 0 || !first ? 1u : 0u);
-              };
-              if (!__all_sync(0xffffffffu, mbar_wait(&p_half[s], ph, p.err, 128))) { ok = false; break; }
-              tc_fence_after();
-              if (elect_one()) half(0);
-              __syncwarp();
               if (!__all_sync(0xffffffffu, mbar_wait(&p_ready[s], ph, p.err, 117))) { ok = false; break; }
               ph ^= 1u;
               tc_fence_after();
               if (elect_one()) {
-                half(4);
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                  mma_bf16_ts(tmem_u + C::COL_O + (uint32_t)(s * DHP), tmem_u + C::COL_S + (uint32_t)(s * 128 + kk * 8), dv + ((kk * 2048) >> 4), idesc,
+                              kk != 0 || !first ? 1u : 0u);
                 mma_commit(&pv_done[s]);
-                if (!C::OWN_P) {
-                  tc_fence_before();
-                  mbar_arrive(&s_free[s]);
-                }
+                tc_fence_before();
+                mbar_arrive(&s_free[s]);
               }
               first = false;
               __syncwarp();
@@ -379,13 +289,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               uint4* piece = reinterpret_cast<uint4*>(tile + (i >> 10) * C::SUB + (i & 1023) * 16);
               uint4 x = make_uint4(0, 0, 0, 0);
               if (r < n) {
-                x = *piece;
-                uint32_t* u = reinterpret_cast<uint32_t*>(&x);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  if ((u[e] & 0x7f80u) == 0x7f80u) u[e] &= 0xffff0000u;
-                  if ((u[e] & 0x7f800000u) == 0x7f800000u) u[e] &= 0xffffu;
-                }
+                x = seq_finite8(*piece);
               }
               *piece = x;
             }
@@ -412,35 +316,14 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     const int r = q * 32 + lane;                             // stacked row
     const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16);
     const uint32_t s_addr = lane_addr + C::COL_S + (uint32_t)s * 128, o_addr = lane_addr + C::COL_O + (uint32_t)(s * DHP);
-    const uint32_t p_addr = lane_addr + C::COL_P + (uint32_t)s * C::P_STEP;
     const uint32_t other = lane_addr + C::COL_O + (uint32_t)((s ^ 1) * DHP);
     const float scale = p.scale_log2;
-    // 4 x 4 transpose of 16-byte pieces inside each group of four lanes: lane 4j + i then holds piece i of rows 4j .. 4j + 3, so that
-    // every store instruction writes whole 64-byte parts of rows
-    auto xchg = [&](uint4& keep_lo, uint4& keep_hi, bool upper, int dist) {
-      // lanes with `upper` clear give away keep_hi and receive into it; lanes with it set give away keep_lo
-      uint4 send = upper ? keep_lo : keep_hi, recv;
-      recv.x = __shfl_xor_sync(0xffffffffu, send.x, dist); recv.y = __shfl_xor_sync(0xffffffffu, send.y, dist);
-      recv.z = __shfl_xor_sync(0xffffffffu, send.z, dist); recv.w = __shfl_xor_sync(0xffffffffu, send.w, dist);
-      if (upper) keep_lo = recv; else keep_hi = recv;
-    };
-    auto transpose4 = [&](uint4 (&t)[4]) {
-      xchg(t[0], t[1], (lane & 1) != 0, 1);
-      xchg(t[2], t[3], (lane & 1) != 0, 1);
-      xchg(t[0], t[2], (lane & 2) != 0, 2);
-      xchg(t[1], t[3], (lane & 2) != 0, 2);
-    };
-    // scores with this maximum against reference m, or against 0 where there was none yet: 2^(score - m) leaves the range that bf16 and
-    // fp32 sums are safe in
-    auto too_far = [](float top, float m) { return m == -INFINITY ? top < -kSeqBelow || top > kSeqAbove : top > m + kSeqAbove; };
     bool ok = true;
     uint32_t s_ph = 0, pv_ph = 0, joined = 0;                // pv_ph: of the slot's next value contraction; joined: items with joined slots
     for (int pass = 0; pass < 2; ++pass) {
       for (SeqWalk at(p, s_bad, pass > 0); ok && at.work >= 0; at.next(p, s_bad, pass > 0)) {
         bool valid, any_valid, mine = false;                 // mine: the slot took a tile, its accumulator holds something
-        // m: reference of the row (log2 domain) in use, m_next: from the next tile on, l: sum so far
-        float m = -INFINITY, m_next = m, l = 0.f;
-        bool far = false;
+        float m = -INFINITY, l = 0.f;
         // What the tile loop needs of the item, in few registers (a tile's scores take 128); the rest is read again behind it.
         int t, end, step, n_tree, vis, anc, first_row, first_top = 0;       // vis: keys (history) or cached rows (tree) that the row sees
         {
@@ -459,12 +342,13 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           s_ph ^= 1u;
           if (any_valid) {
             tc_fence_after();
-            const bool new_rows = TREE && t < n_tree;
-            const int n = vis - (t - n_tree) * 128;          // keys of the tile that the row sees
-            bool masked = __any_sync(0xffffffffu, n < 128);
-            uint32_t see[4] = {0u, 0u, 0u, 0u};
-            if (new_rows) {
+            float v[128];
+#pragma unroll
+            for (int c = 0; c < 128; c += 32) tmem_ld_32x32(s_addr + c, *reinterpret_cast<float(*)[32]>(&v[c]));
+            tmem_wait_ld();
+            if (TREE && t < n_tree) {
               const int j0 = (first_top - t) * 128;
+              uint32_t see[4] = {0u, 0u, 0u, 0u};
               while (anc >= j0 + 128) anc = seq_parent(p, first_row, anc);
               while (anc >= j0) {
                 const int b = anc - j0;
@@ -472,44 +356,30 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 for (int i = 0; i < 4; ++i) see[i] |= (b >> 5) == i ? 1u << (b & 31) : 0u;
                 anc = seq_parent(p, first_row, anc);
               }
-              __syncwarp();
-            } else if (masked) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) { const int left = n - 32 * i; see[i] = left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u; }
-            }
-            masked |= new_rows;
-            auto mask32 = [&](float (&v)[32], uint32_t bits) {
-              if (masked) {
+              for (int j = 0; j < 128; ++j)
+                if (((see[j >> 5] >> (j & 31)) & 1u) == 0) v[j] = -INFINITY;
+            } else {
+              const int n = vis - (t - n_tree) * 128;                            // keys of the tile that the row sees
+              if (__any_sync(0xffffffffu, n < 128)) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                  if (((bits >> j) & 1u) == 0) v[j] = -INFINITY;
+                for (int j = 0; j < 128; ++j)
+                  if (j >= n) v[j] = -INFINITY;
               }
-            };
-            auto most32 = [&](const float (&v)[32], float mx) {
-              float a = v[0], b = v[1];
-#pragma unroll
-              for (int j = 2; j < 30; j += 4) { a = seq_max3(a, v[j], v[j + 2]); b = seq_max3(b, v[j + 1], v[j + 3]); }
-              return seq_max3(fmaxf(mx, v[30]), fmaxf(a, v[31]), b);
-            };
-            if (pass > 0) {
-              // The second time the maximum is known first.  It is taken where the reference would be too far off, and only there: whatever
-              // the item is done again for, the other rows come out as they did.
-              float mx = -INFINITY;
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                float v[32];
-                tmem_ld_32x32(s_addr + 32 * c, v);
-                tmem_wait_ld();
-                mask32(v, see[c]);
-                mx = most32(v, mx);
-              }
-              if (mx != -INFINITY && too_far(mx * scale, m_next)) m_next = mx * scale;
             }
-            const bool raise = valid && m_next != m;
-            if (mine && __any_sync(0xffffffffu, raise)) {
+            float mx0 = v[0], mx1 = v[1], mx2 = v[2], mx3 = v[3];
+#pragma unroll
+            for (int j = 4; j < 128; j += 4) {
+              mx0 = fmaxf(mx0, v[j]); mx1 = fmaxf(mx1, v[j + 1]); mx2 = fmaxf(mx2, v[j + 2]); mx3 = fmaxf(mx3, v[j + 3]);
+            }
+            const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+            // raise the reference only when it is exceeded by more than the threshold, or unset
+            const bool need = valid && (mx - m) * scale > kSeqRescale;
+            const float m_new = need ? mx : m;
+            const float factor = need && m != -INFINITY ? seq_ex2((m - m_new) * scale) : 1.f;
+            if (mine && __any_sync(0xffffffffu, need)) {
               if (!__all_sync(0xffffffffu, mbar_wait(&pv_done[s], pv_ph ^ 1u, p.err, 121))) { ok = false; break; }
               tc_fence_after();
-              const float factor = raise && m != -INFINITY ? seq_ex2(m - m_next) : 1.f;
 #pragma unroll 1
               for (int c = 0; c < DHP; c += 32) {
                 float a[32];
@@ -519,79 +389,29 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 for (int j = 0; j < 32; ++j) a[j] *= factor;
                 tmem_st_32x32(o_addr + c, a);
               }
-              l *= factor;
             }
-            m = m_next;
-            const float ref = m == -INFINITY ? 0.f : m;
-            float mx = -INFINITY;
+            l *= factor;
+            m = m_new;
+            const float ref = m == -INFINITY ? 0.f : m * scale;
             float2 s0 = make_float2(0.f, 0.f), s1 = s0;
             const float2 sc2 = make_float2(scale, scale), rf2 = make_float2(-ref, -ref);
-            // 32 keys of the tile: probabilities, their sum, the maximum
-            auto chunk = [&](float (&x)[32], uint32_t bits, uint32_t to, bool first) {
-              mask32(x, bits);
+#pragma unroll
+            for (int c = 0; c < 128; c += 32) {
               float packed[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) {
-                float2 e = __ffma2_rn(make_float2(x[2 * j], x[2 * j + 1]), sc2, rf2);
+                float2 e = __ffma2_rn(make_float2(v[c + 2 * j], v[c + 2 * j + 1]), sc2, rf2);
                 e = make_float2(seq_ex2(e.x), seq_ex2(e.y));
                 if (j & 1) s1 = __fadd2_rn(s1, e); else s0 = __fadd2_rn(s0, e);
                 packed[j] = __uint_as_float(seq_pack(e.x, e.y));
               }
-              mx = most32(x, mx);
-              if (C::OWN_P && first && mine) {               // the last probabilities are read
-                ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[s], pv_ph ^ 1u, p.err, 129));
-                tc_fence_after();
-              }
-              tmem_st_32x16(to, packed);
-            };
-            // Rolled up: unrolled over the tile, the code of the roles does not stay in the instruction caches (twice the time).
-            float x0[32], x1[32];
-            tmem_ld_32x32(s_addr, x0);
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-              tmem_wait_ld();
-              tmem_ld_32x32(s_addr + 64 * h + 32, x1);
-              chunk(x0, h ? see[2] : see[0], p_addr + 32 * h, h == 0);
-              tmem_wait_ld();
-              if (h == 0) {
-                tmem_ld_32x32(s_addr + 64, x0);
-              } else if (C::OWN_P) {                         // all scores are in registers
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&s_free[s]);
-                __syncwarp();                                // (the whole warp loads from and stores to tensor memory)
-              }
-              chunk(x1, h ? see[3] : see[1], p_addr + 32 * h + 16, false);
-              if (h == 0) {
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_half[s]);
-                __syncwarp();
-              }
+              tmem_st_32x16(s_addr + (uint32_t)(c >> 1), packed);
             }
             s0 = __fadd2_rn(s0, s1);
             l += s0.x + s0.y;
-            // the reference of the next tile
-            const float top = mx * scale;
-            if (mx != -INFINITY) {
-              far |= too_far(top, m);
-              if (m == -INFINITY) {
-                m = 0.f;
-                m_next = fabsf(top) > kSeqRescale ? top : 0.f;
-              } else {
-                m_next = top > m + kSeqRescale ? top : m;
-              }
-            }
             tmem_wait_st();
             tc_fence_before();
-          } else {
-            // a warp without rows keeps step: with scores ahead of the probabilities it could else arrive for a tile too early
-            if (lane == 0 && C::OWN_P) mbar_arrive(&s_free[s]);
-            if (C::OWN_P && mine) ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[s], pv_ph ^ 1u, p.err, 130));
-            if (lane == 0) mbar_arrive(&p_half[s]);
           }
-          if (!ok) break;
           __syncwarp();
           if (lane == 0) mbar_arrive(&p_ready[s]);
           pv_ph ^= 1u;
@@ -615,7 +435,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           ++joined;
           const float2 o = s_ml[(s ^ 1) * 128 + r];
           const float mm = fmaxf(m, o.x), ref = mm == -INFINITY ? 0.f : mm;
-          w0 = seq_ex2(m - ref); w1 = seq_ex2(o.x - ref);
+          w0 = seq_ex2((m - ref) * scale); w1 = seq_ex2((o.x - ref) * scale);
           l = l * w0 + o.y * w1;
           m = mm;
         }
@@ -626,17 +446,14 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           const int64_t part = (int64_t)w.it.part * p.Hkv + kvh;
           const int R = p.tok * G, pr = w.first_token(s) * G + r;
           if (!whole && valid && (s == 0 || !w.same)) {
-            p.part_ml[part * 2 * R + pr] = m;
+            p.part_ml[part * 2 * R + pr] = m == -INFINITY ? m : m * scale;
             p.part_ml[(part * 2 + 1) * R + pr] = l;
           }
           const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
           w0 *= inv; w1 *= inv;
           // where this row goes (element offset in the output, or in the partial results); -1: nowhere
           const int64_t to = !valid ? -1 : whole ? (int64_t)(w.it.row0 + tok) * p.out_stride + (kvh * G + r % G) * p.dh : (part * R + pr) * p.dh;
-          int64_t to4[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) to4[i] = __shfl_sync(0xffffffffu, to, (lane & ~3) + i);
-          float z = pass > 0 ? 0.f : far ? 1.f : l * 0.f;         // not 0: not finite, or too far from the reference
+          float z = 0.f;
 #pragma unroll 1
           for (int c = c_lo; c < c_hi; c += 32) {
             float a[32];
@@ -654,37 +471,14 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
               for (int j = 0; j < 32; ++j) a[j] = fmaf(b[j], w1, a[j]);
             }
             if (pass > 0) {
-              if (valid) seq_add_not_finite<TREE>(p, w, tok, kvh, w.same || s == 1 ? w.it.t0 : w.lo0, w.same || s == 1 ? w.it.t1 : w.hi0, c, a);
+              if (valid) seq_add_not_finite<TREE>(p, at.work, tok, w.same ? w.it.t0 : w.first(s), w.end(s), c, a);
               __syncwarp();
             } else {
 #pragma unroll
               for (int j = 0; j < 32; ++j)
                 if (c + (j & ~7) < p.dh) z = fmaf(a[j], 0.f, z);               // 0 * infinity and 0 * NaN
             }
-            if (whole) {
-              uint4 t4[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                t4[i] = make_uint4(seq_pack(a[8 * i], a[8 * i + 1]), seq_pack(a[8 * i + 2], a[8 * i + 3]), seq_pack(a[8 * i + 4], a[8 * i + 5]), seq_pack(a[8 * i + 6], a[8 * i + 7]));
-              transpose4(t4);
-              const int col = c + (lane & 3) * 8;
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (to4[i] >= 0 && col < p.dh) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + to4[i] + col) = t4[i];
-            } else {
-#pragma unroll
-              for (int h = 0; h < 32; h += 16) {
-                uint4 t4[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  t4[i] = make_uint4(__float_as_uint(a[h + 4 * i]), __float_as_uint(a[h + 4 * i + 1]), __float_as_uint(a[h + 4 * i + 2]), __float_as_uint(a[h + 4 * i + 3]));
-                transpose4(t4);
-                const int col = c + h + (lane & 3) * 4;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (to4[i] >= 0 && col < p.dh) *reinterpret_cast<uint4*>(p.part_acc + to4[i] + col) = t4[i];
-              }
-            }
+            seq_store32(p, whole, a, to, c, lane);
           }
           if (__any_sync(0xffffffffu, valid && z != 0.f) && lane == 0) {
             const int bit = min(at.k - 1, 4095);
@@ -717,29 +511,18 @@ template <int DHP, bool TREE>
 static lime_status launch_tc(const SeqParams& p, cudaStream_t st) {
   using C = SeqTcCfg<DHP>;
   static bool set[kMaxDeviceOrdinals] = {};
-  CUtensorMap q, k, v, ck, cv;
-  // maps of tensors that are not there stand on the queries and are not read inside
-  const bool fresh = p.k != nullptr && (TREE ? true : p.kv_rows > 0), pages = TREE && p.n_pages > 0;
-  const uint64_t rows = fresh ? (uint64_t)(TREE ? p.q_rows : p.kv_rows) : 1;
-  bool ok = make_tmap_bf16_heads(&q, p.q, p.Hq, p.dh, (uint64_t)p.q_rows, p.q_stride, p.G, p.tok / 2);
-  ok = ok && make_tmap_bf16_heads(&k, fresh ? p.k : p.q, p.Hkv, p.dh, rows, fresh ? p.k_stride : p.q_stride, 1, 128);
-  ok = ok && make_tmap_bf16_heads(&v, fresh ? p.v : p.q, p.Hkv, p.dh, rows, fresh ? p.v_stride : p.q_stride, 1, 128);
-  const uint64_t crows = pages ? (uint64_t)(p.n_pages * p.page_rows) : 1;
-  const uint32_t box = TREE ? (uint32_t)(p.page_rows < 128 ? p.page_rows : 128) : 128;
-  ok = ok && make_tmap_bf16_heads(&ck, pages ? p.ck : p.q, p.Hkv, p.dh, crows, (uint64_t)p.Hkv * p.dh, 1, box);
-  ok = ok && make_tmap_bf16_heads(&cv, pages ? p.cv : p.q, p.Hkv, p.dh, crows, (uint64_t)p.Hkv * p.dh, 1, box);
-  if (!ok) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+  SeqMaps m;
+  if (!seq_make_maps(m, p, TREE, p.tok / 2, 128)) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
   const lime_status s = ensure_dynamic_smem((const void*)k_seq_attn_tc<DHP, TREE>, (int)C::SMEM, set);
   if (s != LIME_OK) return s;
   const int64_t work = (int64_t)p.items_upper * p.Hkv;
   ProfScope _p("k_seq_attn_tc", st);
-  launch_pdl(k_seq_attn_tc<DHP, TREE>, dim3((unsigned)(work < kSMs ? work : kSMs)), dim3(C::THREADS), C::SMEM, st, q, k, v, ck, cv, p);
+  launch_pdl(k_seq_attn_tc<DHP, TREE>, dim3((unsigned)(work < kSMs ? work : kSMs)), dim3(C::THREADS), C::SMEM, st, m.q, m.k, m.v, m.ck, m.cv, p);
   LIME_LAUNCH_CHECK("k_seq_attn_tc");
   return LIME_OK;
 }
 
 lime_status launch_seq_attn_tc(const SeqParams& p, bool tree, cudaStream_t st) {
-  if (p.dh <= 64) return tree ? launch_tc<64, true>(p, st) : launch_tc<64, false>(p, st);
   return tree ? launch_tc<128, true>(p, st) : launch_tc<128, false>(p, st);
 }
 

@@ -52,7 +52,7 @@ __device__ __forceinline__ SeqItem seq_row_tile(const SeqParams& p, const int32_
 // shorter (100 users of 0..1000 rows: 22 us by atomics and three lookups in global memory, 8.6 us now, both cold).
 template <bool TREE>
 __global__ void __launch_bounds__(kSeqThreads) k_seq_schedule(const SeqParams p) {
-  __shared__ int s_scan[32], s_near[kSeqNear + 1], s_bin[kSeqBins], s_longest[32];
+  __shared__ int s_scan[32], s_near[kSeqNear + 1], s_bin[kSeqBins], s_longest[32], s_pieces[8], s_len[8];
   __shared__ long long s_work[32];
   __shared__ int s_items, s_parts, s_split;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
@@ -103,7 +103,37 @@ __global__ void __launch_bounds__(kSeqThreads) k_seq_schedule(const SeqParams p)
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) { work += __shfl_xor_sync(0xffffffffu, work, o); longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o)); }
   const long long want = (work * p.Hkv + p.chunk_target - 1) / p.chunk_target;
-  const int chunk = (int)max((long long)p.chunk_min, min(want, (long long)0x7fffffff));
+  int chunk = (int)max((long long)p.chunk_min, min(want, (long long)0x7fffffff));
+  if ((long long)tiles * p.Hkv >= 4 * p.ctas) {
+    chunk = (int)max((long long)chunk, (work * p.Hkv + 2 * p.ctas - 1) / (2 * p.ctas));        // a row tile that is half a CTA's share
+  } else if ((long long)tiles * p.Hkv * ((longest - 1) / chunk + 1) > p.ctas) {
+    // Few row tiles, but more pieces of the least length than run at once: the length that lets the CTAs finish first.  Eight lengths in
+    // equal ratios from the shortest allowed to the longest row tile; with P pieces the end comes after a piece and the cost of an item
+    // where all run at once, else after the CTAs' share of everything and half a piece.  Costs in key tiles.
+    if (tid < 8) {
+      s_pieces[tid] = 0;
+      s_len[tid] = tid == 7 ? longest : min(longest, (int)(chunk * exp2f(log2f((float)longest / chunk) * ((float)tid / 7.f)) + 0.5f));
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < tiles; i += threads) {
+      int l = own.t1;
+      if (i != tid) l = seq_row_tile<TREE>(p, tile_start, i).t1;
+#pragma unroll 1
+      for (int c = 0; c < 8; ++c) atomicAdd(&s_pieces[c], l > s_len[c] ? (l - 1) / s_len[c] + 1 : 1);
+    }
+    __syncthreads();
+    float best = 0.f;
+    int best_len = chunk;
+#pragma unroll 1
+    for (int c = 0; c < 8; ++c) {
+      const int len = s_len[c];
+      const float all = (float)s_pieces[c] * p.Hkv, item = p.item_cost + (s_pieces[c] > tiles ? p.split_cost : 0.f);
+      const float cost = all <= p.ctas ? len + item : ((float)work * p.Hkv + all * item) / p.ctas + 0.5f * (len + item);
+      if (c == 0 || cost < best) { best = cost; best_len = len; }
+    }
+    chunk = best_len;
+  }
   const int bin_width = min(longest, chunk) / kSeqBins + 1;
   for (int i = tid; i < tiles; i += threads) {
     const int len = i == tid ? own.t1 : seq_row_tile<TREE>(p, tile_start, i).t1, ns = len > chunk ? (len - 1) / chunk + 1 : 1;

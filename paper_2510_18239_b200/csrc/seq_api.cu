@@ -21,25 +21,32 @@ static lime_status ready(const Ctx* c) {
 constexpr int64_t kMaxRows = 0x7fff0000LL;       // row indexes and the ends of the tiles that hold them stay inside 32 bits
 
 // How the rows of a batch are tiled, and how fine a batch may be cut (both attention calls).
-struct SeqTiling { int tok, kt, chunk_min, chunk_target; bool few; };
+struct SeqTiling { int tok, kt, chunk_min, chunk_target, ctas; float item_cost, split_cost; bool few; };
 static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows) {
   const int G = c->seq.Hq / c->seq.Hkv;
   SeqTiling t;
   if (c->cfg.dtype == LIME_BF16) {
-    // tensor cores: two slots of 128 stacked rows
-    t.few = false;
-    t.tok = 2 * (128 / G);
-    t.kt = 128;
-    t.chunk_min = 8;
-    t.chunk_target = 3 * kSMs;
+    // tensor cores: 128 stacked rows a CTA and two CTAs an SM, or two slots of 128 rows
+    const bool narrow = c->seq.d_h <= 64;
+    t.few = rows * G <= 64ll * B;                   // partial results of a few rows cost little
+    t.tok = (narrow ? 1 : 2) * (128 / G);
+    t.kt = narrow ? 64 : 128;
+    t.ctas = (narrow ? 2 : 1) * kSMs;
+    t.chunk_min = t.few ? (narrow ? 2 : 4) : narrow ? 8 : 8;
+    t.chunk_target = (t.few ? 8 : 4) * t.ctas;
+    t.item_cost = narrow ? 4.f : 6.f;
+    t.split_cost = t.few ? 1.f : 8.f;
     return t;
   }
   // CUDA cores: 64 stacked rows a tile, or 16 where a user has no more on average
   t.few = G <= 16 && rows * G <= 16ll * B;
   t.tok = (t.few ? 16 : 64) / G;
   t.kt = 64;
-  t.chunk_min = 8;
-  t.chunk_target = 3 * kSMs;
+  t.ctas = kSMs;
+  t.chunk_min = 4;
+  t.chunk_target = 4 * kSMs;
+  t.item_cost = 2.f;
+  t.split_cost = 1.f;
   return t;
 }
 
@@ -49,6 +56,7 @@ static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows) {
 static size_t carve(SeqParams& p, const Ctx* c, int32_t B, int64_t rows, void* base) {
   const SeqTiling t = tiling(c, B, rows);
   p.tok = t.tok; p.kt = t.kt; p.chunk_min = t.chunk_min; p.chunk_target = t.chunk_target;
+  p.ctas = t.ctas; p.item_cost = t.item_cost; p.split_cost = t.split_cost;
   const int64_t R = (int64_t)t.tok * p.G, pieces = 2ll * t.chunk_target / p.Hkv;
   p.row_tiles_upper = (int32_t)(rows / t.tok + (B < rows ? B : rows));
   p.items_upper = (int32_t)(p.row_tiles_upper + pieces);
@@ -88,7 +96,7 @@ static lime_status attend(const Ctx* c, SeqParams& p, bool tree, void* ws, size_
   if ((int64_t)p.items_upper * p.Hkv > 0x7fffffffLL) return LIME_UNSUPPORTED_SHAPE;
   lime_status s;
   if ((s = launch_seq_schedule(p, tree, st)) != LIME_OK) return s;
-  s = c->cfg.dtype == LIME_BF16 ? launch_seq_attn_tc(p, tree, st) : launch_seq_attn_simt(p, tree, tiling(c, p.B, p.q_rows).few, st);
+  s = c->cfg.dtype == LIME_BF16 ? (p.dh <= 64 ? launch_seq_attn_d64_tc(p, tree, st) : launch_seq_attn_tc(p, tree, st)) : launch_seq_attn_simt(p, tree, tiling(c, p.B, p.q_rows).few, st);
   if (s != LIME_OK) return s;
   return may_split ? launch_seq_merge(p, c->cfg.dtype, st) : LIME_OK;
 }

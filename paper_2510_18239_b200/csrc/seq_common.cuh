@@ -42,7 +42,10 @@ struct SeqParams {
   SeqPlan* plan; SeqItem* items; SeqSplit* splits; int32_t* tile_start;
   float *part_ml, *part_acc;             // [part][kvh][2][tok * G] and [part][kvh][tok * G][dh]
   int32_t row_tiles_upper, items_upper, split_upper;
-  int32_t chunk_min, chunk_target;       // key tiles per item at least; items (over all key heads) that a batch should make at least
+  // how row tiles are cut: key tiles per item at least; items (over all key heads) that a batch may make about; CTAs that run at once; what
+  // an item costs besides its key tiles, and what its being one of several adds, in key tiles
+  int32_t chunk_min, chunk_target, ctas;
+  float item_cost, split_cost;
   int32_t* err;
 };
 
@@ -100,7 +103,8 @@ struct NormRotateArgs {
 lime_status launch_norm_rotate(const NormRotateArgs& a, cudaStream_t st);
 lime_status launch_seq_schedule(const SeqParams& p, bool tree, cudaStream_t st);
 lime_status launch_seq_merge(const SeqParams& p, int dtype, cudaStream_t st);
-lime_status launch_seq_attn_tc(const SeqParams& p, bool tree, cudaStream_t st);        // bf16
+lime_status launch_seq_attn_tc(const SeqParams& p, bool tree, cudaStream_t st);        // bf16, d_h > 64
+lime_status launch_seq_attn_d64_tc(const SeqParams& p, bool tree, cudaStream_t st);    // bf16, d_h <= 64
 lime_status launch_seq_attn_simt(const SeqParams& p, bool tree, bool few_rows, cudaStream_t st);                    // fp32
 
 }  // namespace lime
