@@ -32,8 +32,16 @@ __device__ __forceinline__ void cp_async16(void* dst, const void* src, bool ther
   const int n = there ? 16 : 0;
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_u32(dst)), "l"(src), "r"(n) : "memory");
 }
+// a += p * v unless p < 0 (NaN is not): a predicate instead of a branch, of which a masked tile would have one per (row, key)
+__device__ __forceinline__ void fma2_unless_negative(float2& a, float2 p, float2 v) {
+  uint64_t r = *reinterpret_cast<uint64_t*>(&a);
+  asm("{\n\t.reg .pred q;\n\tsetp.geu.f32 q, %1, 0f00000000;\n\t@q fma.rn.f32x2 %0, %2, %3, %0;\n\t}\n"
+      : "+l"(r) : "f"(p.x), "l"(*reinterpret_cast<uint64_t*>(&p)), "l"(*reinterpret_cast<uint64_t*>(&v)));
+  a = *reinterpret_cast<float2*>(&r);
+}
+
 template <int DHP, int RT, bool TREE>
-__global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
+__global__ void __launch_bounds__(256, DHP <= 64 ? 2 : 1) k_seq_attn_simt(const SeqParams p) {
   using C = SimtCfg<DHP, RT>;
   constexpr int LD = C::LD, PLD = C::PLD, KT = kSimtKeys, VW = C::VW, DC = C::DC, RI = C::RI;
   extern __shared__ __align__(16) float sm[];
@@ -53,10 +61,28 @@ __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
     const float* src = static_cast<const float*>(p.q) + (there ? (int64_t)(it.row0 + r / G) * p.q_stride + (kvh * G + r % G) * p.dh + c * 4 : 0);
     cp_async16(sQ + r * LD + c * 4, src, there);
   }
+  // cached rows of the keys that this thread copies of a tile (-1: none): looked up a tile ahead of their copy
+  constexpr int PER = KT * (DHP / 4) / 256;
+  int64_t row_of[PER];
+  auto look_up = [&](int t) {
+    if (!TREE || t >= it.t1) return;
+    const SeqTile s = seq_tile<TREE>(p, it, n_tree, t);
+    if (s.kind != 1) return;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int j = s.j0 + (tid + u * 256) / (DHP / 4);
+      row_of[u] = -1;
+      if (j < s.n) {
+        const int64_t pg = seq_page(p, it.a, j);
+        if (pg < p.n_pages) row_of[u] = (pg * p.page_rows + (j & (p.page_rows - 1))) * p.Hkv + kvh;
+      }
+    }
+  };
   auto fetch = [&](int t, int buf) {
     const SeqTile s = seq_tile<TREE>(p, it, n_tree, t);
-    for (int i = tid; i < KT * (DHP / 4); i += 256) {
-      const int j = i / (DHP / 4), c = i % (DHP / 4);
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int i = tid + u * 256, j = i / (DHP / 4), c = i % (DHP / 4);
       bool there = s.j0 + j < s.n && c < chunks;
       const float *kp = static_cast<const float*>(TREE ? p.q : p.k), *vp = kp;
       if (there) {
@@ -65,12 +91,10 @@ __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
           kp = static_cast<const float*>(p.k) + row * p.k_stride + kvh * p.dh + c * 4;
           vp = static_cast<const float*>(p.v) + row * p.v_stride + kvh * p.dh + c * 4;
         } else {
-          const int64_t pg = seq_page(p, it.a, s.j0 + j);
-          there = pg < p.n_pages;
+          there = row_of[u] >= 0;
           if (there) {
-            const int64_t row = (pg * p.page_rows + ((s.j0 + j) & (p.page_rows - 1))) * p.Hkv + kvh;
-            kp = static_cast<const float*>(p.ck) + row * p.dh + c * 4;
-            vp = static_cast<const float*>(p.cv) + row * p.dh + c * 4;
+            kp = static_cast<const float*>(p.ck) + row_of[u] * p.dh + c * 4;
+            vp = static_cast<const float*>(p.cv) + row_of[u] * p.dh + c * 4;
           }
         }
       }
@@ -89,7 +113,11 @@ __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
   // the row whose mask this thread keeps: its token, and how far up its chain of ancestors it has come
   const int mtok = tid < rows ? tid / G : 0;
   int anc = it.c + mtok;
-  if (it.t0 < it.t1) fetch(it.t0, 0);
+  if (it.t0 < it.t1) {
+    look_up(it.t0);
+    fetch(it.t0, 0);
+    look_up(it.t0 + 1);
+  }
   for (int t = it.t0; t < it.t1; ++t) {
     const int buf = (t - it.t0) & 1;
     const SeqTile s = seq_tile<TREE>(p, it, n_tree, t);
@@ -113,12 +141,13 @@ __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
     }
     __syncthreads();
     if (t + 1 < it.t1) fetch(t + 1, buf ^ 1);
+    look_up(t + 2);
     const float *kb = sK + buf * KT * LD, *vb = sV + buf * KT * LD;
-    float sc[RI][4];
+    float2 sc2[RI][4];                               // sums over even and odd features
 #pragma unroll
     for (int i = 0; i < RI; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sc[i][j] = 0.f;
+      for (int j = 0; j < 4; ++j) sc2[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 4
     for (int c = 0; c < DHP; c += 4) {
       float4 kf[4];
@@ -129,8 +158,8 @@ __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
         const float4 qf = *reinterpret_cast<const float4*>(sQ + (ty + 16 * i) * LD + c);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          sc[i][j] = fmaf(qf.x, kf[j].x, sc[i][j]); sc[i][j] = fmaf(qf.y, kf[j].y, sc[i][j]);
-          sc[i][j] = fmaf(qf.z, kf[j].z, sc[i][j]); sc[i][j] = fmaf(qf.w, kf[j].w, sc[i][j]);
+          sc2[i][j] = __ffma2_rn(make_float2(qf.x, qf.y), make_float2(kf[j].x, kf[j].y), sc2[i][j]);
+          sc2[i][j] = __ffma2_rn(make_float2(qf.z, qf.w), make_float2(kf[j].z, kf[j].w), sc2[i][j]);
         }
       }
     }
@@ -138,12 +167,12 @@ __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
     for (int i = 0; i < RI; ++i) {
       const int r = ty + 16 * i;
       bool sees[4];
-      float mx = -INFINITY;
+      float mx = -INFINITY, sc[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         sees[j] = !masked || ((mask[2 * r + (j >> 1)] >> (tx + 16 * (j & 1))) & 1u) != 0;
-        sc[i][j] = sees[j] ? sc[i][j] * p.scale_log2 : -INFINITY;
-        mx = fmaxf(mx, sc[i][j]);
+        sc[j] = sees[j] ? (sc2[i][j].x + sc2[i][j].y) * p.scale_log2 : -INFINITY;
+        mx = fmaxf(mx, sc[j]);
       }
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -153,7 +182,7 @@ __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float e = exp2f(sc[i][j] - ref);
+        const float e = exp2f(sc[j] - ref);
         if (sees[j]) sum += e;
         sP[r * PLD + tx + 16 * j] = sees[j] ? e : -1.f;
       }
@@ -180,11 +209,15 @@ __global__ void __launch_bounds__(256, 1) k_seq_attn_simt(const SeqParams p) {
             else *reinterpret_cast<float2*>(vf + c * VW) = *reinterpret_cast<const float2*>(src);
           }
 #pragma unroll
-          for (int i = 0; i < RI; ++i)
-            if (!decltype(skip)::value || !(pf[i][jj] < 0.f)) {
+          for (int i = 0; i < RI; ++i) {
 #pragma unroll
-              for (int c = 0; c < DC * VW; ++c) acc[i][c] = fmaf(pf[i][jj], vf[c], acc[i][c]);
+            for (int c = 0; c < DC * VW; c += 2) {
+              float2& a = *reinterpret_cast<float2*>(&acc[i][c]);
+              const float2 pp = make_float2(pf[i][jj], pf[i][jj]), vv = make_float2(vf[c], vf[c + 1]);
+              if constexpr (decltype(skip)::value) fma2_unless_negative(a, pp, vv);
+              else a = __ffma2_rn(pp, vv, a);
             }
+          }
         }
       }
     };

@@ -42,9 +42,9 @@ static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows) {
   t.few = G <= 16 && rows * G <= 16ll * B;
   t.tok = (t.few ? 16 : 64) / G;
   t.kt = 64;
-  t.ctas = kSMs;
+  t.ctas = (c->seq.d_h <= 64 ? 2 : 1) * kSMs;
   t.chunk_min = 4;
-  t.chunk_target = 4 * kSMs;
+  t.chunk_target = 4 * t.ctas;
   t.item_cost = 2.f;
   t.split_cost = 1.f;
   return t;
@@ -93,7 +93,7 @@ static lime_status attend(const Ctx* c, SeqParams& p, bool tree, void* ws, size_
   const bool may_split = tiles > p.chunk_min;
   const int64_t items = may_split ? p.row_tiles_upper * pieces : p.row_tiles_upper;
   if (items < p.items_upper) p.items_upper = (int32_t)items;
-  if ((int64_t)p.items_upper * p.Hkv > 0x7fffffffLL) return LIME_UNSUPPORTED_SHAPE;
+  if ((int64_t)p.items_upper * p.Hkv > kMaxRows) return LIME_UNSUPPORTED_SHAPE;      // (a round of CTAs past the last item stays inside 32 bits)
   lime_status s;
   if ((s = launch_seq_schedule(p, tree, st)) != LIME_OK) return s;
   s = c->cfg.dtype == LIME_BF16 ? (p.dh <= 64 ? launch_seq_attn_d64_tc(p, tree, st) : launch_seq_attn_tc(p, tree, st)) : launch_seq_attn_simt(p, tree, tiling(c, p.B, p.q_rows).few, st);

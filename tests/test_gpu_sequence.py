@@ -184,6 +184,23 @@ def test_long_histories_are_cut_into_parts(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("rise", [0.02, -0.02, 0.5, -0.5])
+def test_scores_that_grow_and_fall(dtype, dh, rise):
+    """Scores that rise or fall along the keys by far more than the range a probability has: the reference moves again and again, or what
+    comes later vanishes.  And a constant offset of all scores, far from zero, changes nothing."""
+    gen = torch.Generator().manual_seed(43)
+    m = lime(dtype, 2, 1, dh, attn_scale=1.0)
+    n = 700
+    q, k, v = rand(gen, n, 2, dh, dtype=dtype), rand(gen, n, 1, dh, dtype=dtype) * 0.25, rand(gen, n, 1, dh, dtype=dtype)
+    q[:, :, 0], k[:, 0, 0] = 1.0, (torch.arange(n) * rise).to(TYPES[dtype])
+    q[:, :, 1], k[:, 0, 1] = 1.0, -300.0
+    out = m.attend_history(q.cuda(), k.cuda(), v.cuda(), off_of([n]))
+    ref, mag, size = so.attend(f64(q), f64(k), f64(v), so.causal(n, n), 1.0)
+    close(out, ref, mag, size, dh, n, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_history_with_strides(dtype):
     gen = torch.Generator().manual_seed(13)
     Hq, Hkv, dh, lens = 4, 2, 32, [70, 1, 33]
@@ -341,6 +358,55 @@ def test_unwritten_cache_rows_have_no_influence(dtype, bad):
         got = m.attend_tree(q, ck.cuda(), cv.cuda(), table.cuda(), ctx, off_of(n), **args)
         others = [0, 2, 4, 5, 6, 7, 8]
         assert torch.equal(got[others], clean[others]) and not torch.isfinite(got[[1, 3]]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_users_and_offsets_past_the_rows(dtype):
+    """More users than the work lists keep near (2048), most of them empty; offsets past the rows given are cut to them."""
+    gen = torch.Generator().manual_seed(47)
+    m = lime(dtype, 2, 1, 32)
+    lens = [0] * 5000
+    for b, n in ((0, 3), (17, 200), (2047, 1), (2048, 70), (4999, 64)):
+        lens[b] = n
+    check_history(m, gen, dtype, 2, 1, 32, lens, lens, 1 / np.sqrt(32), kv_off=False, tail=5)
+    q, k, v = (rand(gen, 40, h, 32, dtype=dtype) for h in (2, 1, 1))
+    off = torch.tensor([0, 30, 90, 1 << 30], dtype=torch.int32).cuda()
+    out = torch.full((40, 2, 32), 7.0, dtype=TYPES[dtype], device="cuda")
+    m.attend_history(q.cuda(), k.cuda(), v.cuda(), off, out=out)
+    for lo, hi in ((0, 30), (30, 40)):
+        ref, mag, size = so.attend(f64(q[lo:hi]), f64(k[lo:hi]), f64(v[lo:hi]), so.causal(hi - lo, hi - lo), 1 / np.sqrt(32))
+        close(out[lo:hi], ref, mag, size, 32, hi - lo, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_graph_serves_other_lengths_than_it_was_captured_with(dtype):
+    """Lengths, tables and trees are device data: a replay reads what stands there then."""
+    gen = torch.Generator().manual_seed(53)
+    Hq, Hkv, dh, page = 4, 2, 64, 16
+    m = lime(dtype, Hq, Hkv, dh)
+    ck, cv, table = paged(gen, [640, 640], page, Hkv, dh, dtype)
+    q, tk, tv = (rand(gen, 12, h, dh, dtype=dtype) for h in (Hq, Hkv, Hkv))
+    d = [t.cuda() for t in (q, ck, cv, table, tk, tv)]
+    ctx, off = torch.tensor([1, 1], dtype=torch.int32).cuda(), off_of([1, 1])
+    parent = torch.full((12,), -1, dtype=torch.int32, device="cuda")
+    run = lambda: m.attend_tree(d[0], d[1], d[2], d[3], ctx, off, parent=parent, tree_k=d[4], tree_v=d[5])
+    run()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = run()
+    for n, c, par in (([3, 9], [640, 5], [-1, 0, 1] + [-1, 0, 0, 1, 1, 2, 5, -1, 7]), ([0, 12], [0, 600], [-1] + list(range(11))), ([12, 0], [77, 640], [-1] * 12)):
+        off.copy_(off_of(n))
+        ctx.copy_(torch.tensor(c, dtype=torch.int32))
+        parent.copy_(torch.tensor(par, dtype=torch.int32))
+        g.replay()
+        i = 0
+        for b, (a, cb) in enumerate(zip(n, c)):
+            kk = np.concatenate((so.cached_rows(f64(ck), table[b].tolist(), cb), f64(tk[i:i + a])))
+            vv = np.concatenate((so.cached_rows(f64(cv), table[b].tolist(), cb), f64(tv[i:i + a])))
+            sees = np.concatenate((np.ones((a, cb), bool), so.ancestors(par[i:i + a])), 1)
+            ref, mag, size = so.attend(f64(q[i:i + a]), kk, vv, sees, 1 / 8)
+            close(out[i:i + a], ref, mag, size, dh, cb + a, dtype)
+            i += a
 
 
 # ----------------------------------------------------------------------------- the operators together
