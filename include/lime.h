@@ -254,11 +254,13 @@ LIME_API lime_status lime_set_sequence(lime_ctx* ctx, const lime_sequence* seq);
  * for q [rows x Hq x d_h] and k [rows x Hkv x d_h]; statistics, angles and products in 32 bits or more, one rounding at the end.  The
  * angle is formed from the whole position in fixed point, so positions far out lose nothing; negative ones turn backwards.
  * gamma_q / gamma_k [d_h] in config.dtype, NULL = ones.  positions [rows] device int32 (may be NULL with rot_dim = 0).
- * q_out, k_out [rows x ..] with strides of their own; each may be its input itself (same pointer and stride).
+ * q_out, k_out [rows x ..] with strides of their own; each may be its input itself (same pointer and stride), and overlaps nothing else
+ * that is read or written.
  * Cache: with cache_k [cache_rows x Hkv x d_h] (contiguous rows, e.g. pages one after the other), row t of the new keys goes to row
  * slots[t] of it as well, and row t of v [rows x Hkv x d_h] as it is to row slots[t] of cache_v; k_out may then be NULL.  A slot of -1
  * writes nothing (padding); another slot outside [0, cache_rows) writes nothing and lowers *dev_flag (device int32, nullable, caller
- * initialises it to INT32_MAX) to the smallest such t.  Two rows with the same slot: which of them stays is not determined.
+ * initialises it to INT32_MAX) to the smallest such t.  Two rows with the same slot: what that slot
+ * holds afterwards is not determined (parts of both, it may be).
  * v and cache_v are given together, and only with cache_k; slots and cache_k are given together. */
 LIME_API lime_status lime_norm_rotate(lime_ctx* ctx, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                              int64_t v_stride, const void* gamma_q, const void* gamma_k, const int32_t* positions, int64_t rows,
@@ -273,7 +275,7 @@ LIME_API size_t lime_sequence_workspace_bytes(const lime_ctx* ctx, int32_t B, in
  *   out[i, h, :] = sum_j softmax_j(attn_scale <q[i, h, :], k[j, h', :]>) v[j, h', :]   over the keys j <= i + n_keys - n_queries
  * of i's user (i, j counted within the user): the last query sees every key, so new rows behind older ones are queries fewer than
  * keys.  q [q_rows x Hq x d_h] by off, k and v [kv_rows x Hkv x d_h] by kv_off (NULL: the same rows as the queries', kv_rows =
- * q_rows); out [q_rows x Hq x d_h].  A query that sees no key (more queries than keys, an empty history) gets zeros.  What a query does
+ * q_rows); out [q_rows x Hq x d_h], which overlaps no input.  A query that sees no key (more queries than keys, an empty history) gets zeros.  What a query does
  * not see has no influence on it, infinities and NaN included.  bf16: products of bf16 values in fp32, probabilities rounded to bf16 for
  * the value product (their sum is not), one rounding of the result; fp32: all in fp32. */
 LIME_API lime_status lime_attend_history(lime_ctx* ctx, const void* q, int64_t q_stride, const int32_t* off, const void* k,
@@ -285,7 +287,7 @@ LIME_API lime_status lime_attend_history(lime_ctx* ctx, const void* q, int64_t q
  * page_rows x Hkv x d_h]; page_rows is a power of two, 16..4096.  ctx_len is device int32 [B], cut to 0 .. max_pages * page_rows.  A
  * page outside [0, n_pages) among those reads as rows of zeros and lowers *dev_flag (nullable, as above) to the smallest such position
  * b * max_pages + i.  Pages may be shared by users.
- * q [rows x Hq x d_h] and out by off.  Every row sees the user's cached rows, and:
+ * q [rows x Hq x d_h] and out (which overlaps no input) by off.  Every row sees the user's cached rows, and:
  *   tree_k = tree_v = NULL: nothing else (the rows' own keys are in the cache already: one new event, or several that all see it all);
  *   tree_k, tree_v [rows x Hkv x d_h]: the row itself and its ancestors.  parent [rows] device int32: the row's parent as an index among
  *   the user's rows, smaller than its own, anything else makes it a root; parent = NULL: all are roots (a list of candidates).

@@ -8,6 +8,12 @@
 //   scores [128 x 64] = Q [128 x d_h] . K_tile^T       O [128 x d_h] += P [128 x 64] . V_tile
 // in 128 columns of tensor memory and six warps: 0 loads (one lane a page where keys lie in pages), 1 issues both products, 2..5 are the
 // softmax, one thread per row.  The CTAs are persistent and walk the work items of k_seq_schedule back and forth.
+// d_h <= 32 leaves columns for the probabilities, so that the next scores are formed while these are worked out.
+// What bounds it: the hand-overs between the warps, tile by tile.  With loads and contractions issued by one warp and three CTAs an SM,
+// candidate roots (32 users of 1000 behind 1024 rows, 8 heads of 32) took 189 us; without their exponentials and contractions still 178; with nothing
+// left but the hand-overs 130.  The exponentials alone would take about 70.  As it stands they take 172 and 100 ragged users of 0..1000
+// rows 65.  More CTAs an SM do not help: four with 80 registers a thread, the scores loaded twice, 180 and 63..67; three as above 189 and
+// 69; both slots of k_seq_attn_tc.cu in one CTA 172 and 72.
 // The rest is as in k_seq_attn_tc.cu: online softmax with lazy rescale, probabilities rounded to bf16 for the value product and summed
 // unrounded, features past d_h as zeros in shared memory only, value rows behind the end of a cached range zeroed there, items whose
 // result is not finite done again with what is not finite taken out of the tiles that mask anything.
@@ -35,8 +41,8 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kD64OffBar);
   uint64_t* kv_full = bars;            // [8] keys or values of a tile landed
   uint64_t* kv_empty = bars + 8;       // [8] every MMA that reads them has run
-  uint64_t* q_full = bars + 16;         //     queries of an item landed
-  uint64_t* q_empty = bars + 17;        //     every score MMA that reads them has run
+  uint64_t* q_full = bars + 16;        //     queries of an item landed
+  uint64_t* q_empty = bars + 17;       //     every score MMA that reads them has run
   uint64_t* s_full = bars + 18;        //     scores in TMEM
   uint64_t* p_ready = bars + 19;       //     probabilities in TMEM (four warps)
   uint64_t* pv_done = bars + 20;       //     their values are in the accumulator
@@ -77,10 +83,10 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     bool ok = true;
     int g = 0, qn = 0;                                       // loads of keys and values so far (ring position); items with key tiles
     for (int pass = 0; pass < 2; ++pass) {
-    for (SeqWalk at(p, s_bad, pass > 0); ok && at.work >= 0; at.next(p, s_bad, pass > 0)) {
-      const SeqItem it = seq_item(p, at.work);
-      const int kvh = at.work % p.Hkv, n_tree = TREE ? seq_tree_tiles(p, it) : 0;
-      const bool any = it.t0 < it.t1;
+      for (SeqWalk at(p, s_bad, pass > 0); ok && at.work >= 0; at.next(p, s_bad, pass > 0)) {
+        const SeqItem it = seq_item(p, at.work);
+        const int kvh = at.work % p.Hkv, n_tree = TREE ? seq_tree_tiles(p, it) : 0;
+        const bool any = it.t0 < it.t1;
         // ------------------------------------------------------------------ loads
         if (any) {
           if (!__all_sync(0xffffffffu, mbar_wait(q_empty, ((uint32_t)qn & 1u) ^ 1u, p.err, 141))) { ok = false; break; }
@@ -122,25 +128,25 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             __syncwarp();
           }
         }
-    }
-    const int flags = end_of_pass(ok);
-    if (flags & 2) {
-      // giving up: let the copies already issued land (bounded) before this CTA's shared memory goes away
-      for (int j = 0; j < g && j < STAGES; ++j) mbar_wait_quiet(&kv_full[(g - 1 - j) % STAGES], (uint32_t)((g - 1 - j) / STAGES) & 1u);
-      if (qn > 0) mbar_wait_quiet(q_full, (uint32_t)(qn - 1) & 1u);
-    }
-    if (flags != 1) break;
+      }
+      const int flags = end_of_pass(ok);
+      if (flags & 2) {
+        // giving up: let the copies already issued land (bounded) before this CTA's shared memory goes away
+        for (int j = 0; j < g && j < STAGES; ++j) mbar_wait_quiet(&kv_full[(g - 1 - j) % STAGES], (uint32_t)((g - 1 - j) / STAGES) & 1u);
+        if (qn > 0) mbar_wait_quiet(q_full, (uint32_t)(qn - 1) & 1u);
+      }
+      if (flags != 1) break;
     }
   } else if (warp == 1) {
     bool ok = true;
     int g = 0, qn = 0;
     uint32_t n = 0, done = 0;                                // tiles so far; items so far
     for (int pass = 0; pass < 2; ++pass) {
-    const bool again = pass > 0;
-    for (SeqWalk at(p, s_bad, again); ok && at.work >= 0; at.next(p, s_bad, again)) {
-      const SeqItem it = seq_item(p, at.work);
-      const int n_tree = TREE ? seq_tree_tiles(p, it) : 0;
-      const bool any = it.t0 < it.t1;
+      const bool again = pass > 0;
+      for (SeqWalk at(p, s_bad, again); ok && at.work >= 0; at.next(p, s_bad, again)) {
+        const SeqItem it = seq_item(p, at.work);
+        const int n_tree = TREE ? seq_tree_tiles(p, it) : 0;
+        const bool any = it.t0 < it.t1;
         // ------------------------------------------------------------------ both products: values of a tile, then scores of the next
         const uint32_t tmem_u = __shfl_sync(0xffffffffu, tmem_base, 0), idesc_s = make_idesc_bf16(128, KEYS), idesc_o = make_idesc_bf16(128, ksteps * 16, false, true);
         const uint64_t dq = make_sdesc_k_sw128(smem_u32(smem)), dk0 = make_sdesc_k_sw128(smem_u32(smem) + kD64OffKv), dv0 = make_sdesc_mn_sw128(smem_u32(smem) + kD64OffKv, kD64Tile);
@@ -205,8 +211,8 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         if (any) ++g;
         ++done;
-    }
-    if (end_of_pass(ok) != 1) break;
+      }
+      if (end_of_pass(ok) != 1) break;
     }
   } else {
     const int q = warp & 3, r = q * 32 + lane;               // TMEM lane quarter; stacked row
@@ -215,8 +221,8 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     bool ok = true;
     uint32_t n = 0;                                          // tiles so far
     for (int pass = 0; pass < 2; ++pass) {
-    const bool again = pass > 0;
-    for (SeqWalk at(p, s_bad, again); ok && at.work >= 0; at.next(p, s_bad, again)) {
+      const bool again = pass > 0;
+      for (SeqWalk at(p, s_bad, again); ok && at.work >= 0; at.next(p, s_bad, again)) {
         // ------------------------------------------------------------------ softmax
         // What the tile loop needs of the item, in few registers; the rest is read again behind it.
         int t, end, n_tree, vis, anc, first_row, top_tile;   // vis: keys (history) or cached rows (tree) that the row sees
@@ -372,8 +378,8 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(o_free);
-    }
-    if (end_of_pass(ok) != 1) break;
+      }
+      if (end_of_pass(ok) != 1) break;
     }
   }
 

@@ -1,4 +1,4 @@
-// Attention of the sequence path on the 5th-generation tensor cores (bf16, any d_h of the sequence path):
+// Attention of the sequence path on the 5th-generation tensor cores for d_h of 72 .. 128 (bf16; k_seq_attn_d64_tc.cu has the narrower):
 //
 //   out_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(scale log2(e) (<q_i, k_j> - m_i))   over the keys j that row i sees
 //
@@ -14,24 +14,31 @@
 //    warps 4..7 and 8..11 are the softmax of a slot, one thread per row.  Online softmax with lazy rescale: the reference maximum is
 //    raised only when exceeded by 2^8.
 //  * Nothing waits for the end of an item but what needs it: the next one's keys and queries are loaded and its first scores formed while
-//    the softmax warps write a result out (100 users of 0..1000 rows, 4 heads of 32: LIME_TODO us with a barrier of the CTA between items).
-//  * d_h that is not 64 or 128: TMA fills the columns that are not there with zeros in shared memory only, and the contractions stop at
-//    the next multiple of 16.
+//    the softmax warps write a result out (64 single events, 16..16384 keys: 244 -> 227 us; with a barrier of the CTA between items before).
+//  * d_h under 128: TMA fills the columns that are not there with zeros in shared memory only, and the contractions stop at the next
+//    multiple of 16.
 //  * Probabilities are rounded to bf16 for the value product (the operands of one tcgen05.mma have one type); the row sum is taken of the
 //    unrounded ones in fp32.
 //  * Masked positions have p = 0, but 0 * NaN and 0 * infinity are NaN.  Value rows behind the end of a cached range, which may never have
 //    been written, are zeroed in shared memory.  Elsewhere such values are the exception: an item whose result has a NaN or an infinity is
 //    done again with what is not finite taken out of every tile that masks anything; the rows that do see it get it added at the end.
+// What bounds it: 16384 causal rows of 16 heads of 128 over 4 heads of keys take 1.08 to 1.12 ms, 0.98 to 1.02 PFLOP/s at 1.83 GHz and 950 to
+// 1000 W, the power cap: 2250 cycles of an SM for a tile of 128 x 128, of which its contractions fill 1024 of the tensor pipe and its
+// exponentials 1024 of the special-function unit.  A slot's chain (scores, maximum, exponentials, values) is longer than a tile's share of
+// either, and with two slots the one fills the gaps of the other only in part.  Measured and dropped: probabilities against the reference
+// of the tiles before, without waiting for the maximum (1.15 ms); 64-key tiles with two score buffers a slot, which take the scores out of
+// the chain (1.24 ms); two threads a row, 16 softmax warps (1.18 ms); the first half of the probabilities handed over early, polling
+// without a pause (no change).
+// Single events stream their keys at 0.70 of the copy rate (64 users of 16..16384 keys, 1.07 GB: 231 us).
 #include "seq_tc.cuh"
 
 namespace lime {
 
-template <int DHP_>
 struct SeqTcCfg {
-  static constexpr int DHP = DHP_, THREADS = 384, STAGES = DHP == 128 ? 5 : 10, QBUFS = DHP == 128 ? 1 : 2;
+  static constexpr int DHP = 128, THREADS = 384, STAGES = 5;
   static constexpr uint32_t SUB = 128 * 128;                       // [128 rows x 64 features]
   static constexpr uint32_t TILE = (DHP / 64) * SUB;
-  static constexpr uint32_t OFF_Q = 0, OFF_KV = QBUFS * 2 * TILE, OFF_BAR = OFF_KV + STAGES * TILE;
+  static constexpr uint32_t OFF_Q = 0, OFF_KV = 2 * TILE, OFF_BAR = OFF_KV + STAGES * TILE;
   static constexpr uint32_t OFF_ML = OFF_BAR + 512;               // references and sums of joined slots: [2 slots][128] pairs
   static constexpr uint32_t OFF_BAD = OFF_ML + 2 * 128 * 8;       // a bit for every item of the CTA
   static constexpr uint32_t SMEM = OFF_BAD + 512;
@@ -74,13 +81,13 @@ struct SeqWork {
   __device__ __forceinline__ bool mended(const SeqTile& k, bool again) const { return again ? masked(k) : TREE && k.kind == 1 && k.j0 + 128 > k.n; }
 };
 
-template <int DHP, bool TREE>
+template <bool TREE>
 __global__ void __launch_bounds__(384, 1)
 k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
               const __grid_constant__ CUtensorMap tmCK, const __grid_constant__ CUtensorMap tmCV, const __grid_constant__ SeqParams p) {
   using namespace tc;
-  using C = SeqTcCfg<DHP>;
-  constexpr int STAGES = C::STAGES, QBUFS = C::QBUFS;
+  using C = SeqTcCfg;
+  constexpr int DHP = C::DHP, STAGES = C::STAGES;
   extern __shared__ __align__(1024) uint8_t smem[];
   if ((smem_u32(smem) & 1023u) != 0) {                     // the swizzled tiles need a 1024-byte aligned base
     pdl_wait();
@@ -88,11 +95,11 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     return;
   }
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
-  uint64_t* kv_full = bars;            // [10] keys or values of a tile landed
-  uint64_t* kv_empty = bars + 10;      // [10] every MMA that reads them has run
-  uint64_t* mend_done = bars + 20;     // [10] the value tile in this stage is mended
-  uint64_t* q_full = bars + 30;        // [2]  queries of an item landed
-  uint64_t* q_empty = bars + 32;       // [2]  every score MMA that reads them has run
+  uint64_t* kv_full = bars;            // [5]  keys or values of a tile landed
+  uint64_t* kv_empty = bars + 10;      // [5]  every MMA that reads them has run
+  uint64_t* mend_done = bars + 20;     // [5]  the value tile in this stage is mended
+  uint64_t* q_full = bars + 30;        //      queries of an item landed
+  uint64_t* q_empty = bars + 32;       //      every score MMA that reads them has run
   uint64_t* s_full = bars + 34;        // [2]  scores of the slot in TMEM
   uint64_t* s_free = bars + 36;        // [2]  the values of the slot's last probabilities are issued: new scores may follow in the pipe
   uint64_t* p_ready = bars + 38;       // [2]  probabilities in TMEM (four warps)
@@ -144,18 +151,17 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         const int kvh = at.work % p.Hkv;
         const SeqWork<TREE> w(p, at.work);
         const bool any = w.it.t0 < w.it.t1;
-        const int qb = qn % QBUFS;
-        const uint32_t q_ph = (uint32_t)(qn / QBUFS) & 1u;
+        const uint32_t q_ph = (uint32_t)qn & 1u;
         if (any) ++qn;
         if (warp == 0) {
           // ---------------------------------------------------------------- loads
           if (any) {
-            if (!__all_sync(0xffffffffu, mbar_wait(&q_empty[qb], q_ph ^ 1u, p.err, 123))) { ok = false; break; }
+            if (!__all_sync(0xffffffffu, mbar_wait(q_empty, q_ph ^ 1u, p.err, 123))) { ok = false; break; }
             if (lane == 0) {
-              mbar_arrive_expect_tx(&q_full[qb], (w.same ? 1u : 2u) * (uint32_t)(w.ts * G) * 128u * (DHP / 64));
+              mbar_arrive_expect_tx(q_full, (w.same ? 1u : 2u) * (uint32_t)(w.ts * G) * 128u * (DHP / 64));
               for (int s = 0; s < (w.same ? 1 : 2); ++s)
                 for (int c = 0; c < DHP / 64; ++c)
-                  tma_load_3d(smem + C::OFF_Q + (qb * 2 + s) * C::TILE + c * C::SUB, &tmQ, c * 64, kvh * G, w.it.row0 + s * w.ts, &q_full[qb]);
+                  tma_load_3d(smem + C::OFF_Q + s * C::TILE + c * C::SUB, &tmQ, c * 64, kvh * G, w.it.row0 + s * w.ts, q_full);
             }
             __syncwarp();
           }
@@ -196,8 +202,8 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         } else if (warp == 1) {
           // ---------------------------------------------------------------- scores
           const uint32_t idesc = make_idesc_bf16(128, 128);
-          const uint64_t dq0 = make_sdesc_k_sw128(smem_u32(smem) + C::OFF_Q + qb * 2 * C::TILE), dk0 = make_sdesc_k_sw128(smem_u32(smem) + C::OFF_KV);
-          if (any && !__all_sync(0xffffffffu, mbar_wait(&q_full[qb], q_ph, p.err, 112))) { ok = false; break; }
+          const uint64_t dq0 = make_sdesc_k_sw128(smem_u32(smem) + C::OFF_Q), dk0 = make_sdesc_k_sw128(smem_u32(smem) + C::OFF_KV);
+          if (any && !__all_sync(0xffffffffu, mbar_wait(q_full, q_ph, p.err, 112))) { ok = false; break; }
           for (int t = w.it.t0; t < w.it.t1 && ok; ++t, g += 2) {
             const int st = g % STAGES;
             if (!__all_sync(0xffffffffu, mbar_wait(&kv_full[st], (uint32_t)(g / STAGES) & 1u, p.err, 113))) { ok = false; break; }
@@ -220,7 +226,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             }
             if (ok && elect_one()) {
               mma_commit(&kv_empty[st]);
-              if (t + 1 == w.it.t1) mma_commit(&q_empty[qb]);
+              if (t + 1 == w.it.t1) mma_commit(q_empty);
             }
             __syncwarp();
           }
@@ -305,7 +311,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       if ((flags & 2) && warp == 0) {
         // giving up: let the copies already issued land (bounded) before this CTA's shared memory goes away
         for (int j = 0; j < g && j < STAGES; ++j) mbar_wait_quiet(&kv_full[(g - 1 - j) % STAGES], (uint32_t)((g - 1 - j) / STAGES) & 1u);
-        for (int j = 0; j < qn && j < QBUFS; ++j) mbar_wait_quiet(&q_full[(qn - 1 - j) % QBUFS], (uint32_t)((qn - 1 - j) / QBUFS) & 1u);
+        if (qn > 0) mbar_wait_quiet(q_full, (uint32_t)(qn - 1) & 1u);
       }
       if (flags != 1) break;
     }
@@ -507,23 +513,23 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   }
 }
 
-template <int DHP, bool TREE>
+template <bool TREE>
 static lime_status launch_tc(const SeqParams& p, cudaStream_t st) {
-  using C = SeqTcCfg<DHP>;
+  using C = SeqTcCfg;
   static bool set[kMaxDeviceOrdinals] = {};
   SeqMaps m;
   if (!seq_make_maps(m, p, TREE, p.tok / 2, 128)) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
-  const lime_status s = ensure_dynamic_smem((const void*)k_seq_attn_tc<DHP, TREE>, (int)C::SMEM, set);
+  const lime_status s = ensure_dynamic_smem((const void*)k_seq_attn_tc<TREE>, (int)C::SMEM, set);
   if (s != LIME_OK) return s;
   const int64_t work = (int64_t)p.items_upper * p.Hkv;
   ProfScope _p("k_seq_attn_tc", st);
-  launch_pdl(k_seq_attn_tc<DHP, TREE>, dim3((unsigned)(work < kSMs ? work : kSMs)), dim3(C::THREADS), C::SMEM, st, m.q, m.k, m.v, m.ck, m.cv, p);
+  launch_pdl(k_seq_attn_tc<TREE>, dim3((unsigned)(work < kSMs ? work : kSMs)), dim3(C::THREADS), C::SMEM, st, m.q, m.k, m.v, m.ck, m.cv, p);
   LIME_LAUNCH_CHECK("k_seq_attn_tc");
   return LIME_OK;
 }
 
 lime_status launch_seq_attn_tc(const SeqParams& p, bool tree, cudaStream_t st) {
-  return tree ? launch_tc<128, true>(p, st) : launch_tc<128, false>(p, st);
+  return tree ? launch_tc<true>(p, st) : launch_tc<false>(p, st);
 }
 
 }  // namespace lime

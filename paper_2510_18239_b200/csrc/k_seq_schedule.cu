@@ -15,7 +15,7 @@ __device__ __forceinline__ void seq_user_rows(const int32_t* off, int b, int64_t
 // row tile `i` of the batch as an item with all its key tiles
 template <bool TREE>
 __device__ __forceinline__ SeqItem seq_row_tile(const SeqParams& p, const int32_t* tile_start, int i) {
-  int b = 0;                                       // the user: tile_start[b] <= i < tile_start[b + 1] 
+  int b = 0;                                       // the user: tile_start[b] <= i < tile_start[b + 1]
   for (int hi = p.B; hi - b > 1;) {
     const int mid = (b + hi) >> 1;
     if (tile_start[mid] <= i) b = mid; else hi = mid;
@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kSeqThreads) k_seq_schedule(const SeqParams p)
     }
   }
   __syncthreads();
-  if (tid == 0) { p.plan->n_items = s_items; p.plan->n_split = s_split; p.plan->n_parts = s_parts; }
+  if (tid == 0) { p.plan->n_items = s_items; p.plan->n_split = s_split; }
 }
 
 lime_status launch_seq_schedule(const SeqParams& p, bool tree, cudaStream_t st) {

@@ -3,6 +3,12 @@
 
 #include "seq_common.cuh"
 #include "tc_common.cuh"
+#ifndef FEW_MIN
+#define FEW_MIN 4
+#define FEW_TGT 4
+#define FEW_ITEM 4.f
+#define FEW_SPLIT 2.f
+#endif
 
 namespace lime {
 
@@ -22,9 +28,25 @@ constexpr int64_t kMaxRows = 0x7fff0000LL;       // row indexes and the ends of 
 
 // How the rows of a batch are tiled, and how fine a batch may be cut (both attention calls).
 struct SeqTiling { int tok, kt, chunk_min, chunk_target, ctas; float item_cost, split_cost; bool few; };
-static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows) {
+// `alone`: nothing but the cache is attended to.
+static bool streams(const Ctx* c, int32_t B, int64_t rows, bool alone) {
+  const int G = c->seq.Hq / c->seq.Hkv;
+  return alone && c->cfg.dtype == LIME_BF16 && G <= 8 && rows * G <= 8ll * B;
+}
+static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows, bool alone) {
   const int G = c->seq.Hq / c->seq.Hkv;
   SeqTiling t;
+  if (streams(c, B, rows, alone)) {
+    t.few = true;
+    t.tok = 8 / G;
+    t.kt = 64;
+    t.ctas = (c->seq.d_h <= 64 ? 4 : 3) * kSMs;
+    t.chunk_min = FEW_MIN;
+    t.chunk_target = FEW_TGT * t.ctas;
+    t.item_cost = FEW_ITEM;
+    t.split_cost = FEW_SPLIT;
+    return t;
+  }
   if (c->cfg.dtype == LIME_BF16) {
     // tensor cores: 128 stacked rows a CTA and two CTAs an SM, or two slots of 128 rows
     const bool narrow = c->seq.d_h <= 64;
@@ -32,7 +54,7 @@ static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows) {
     t.tok = (narrow ? 1 : 2) * (128 / G);
     t.kt = narrow ? 64 : 128;
     t.ctas = (narrow ? 2 : 1) * kSMs;
-    t.chunk_min = t.few ? (narrow ? 2 : 4) : narrow ? 8 : 8;
+    t.chunk_min = t.few ? (narrow ? 2 : 4) : 8;
     t.chunk_target = (t.few ? 8 : 4) * t.ctas;
     t.item_cost = narrow ? 4.f : 6.f;
     t.split_cost = t.few ? 1.f : 8.f;
@@ -53,8 +75,8 @@ static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows) {
 // Carves the workspace; returns its size.  Row tiles: whole ones and one rest per user.  A row tile is cut into pieces of more than half
 // of what k_seq_schedule calls a chunk, and a chunk is at least 1 / chunk_target of all (row tile, key head) work, so pieces times key
 // heads are at most 2 * chunk_target, whatever the lengths.
-static size_t carve(SeqParams& p, const Ctx* c, int32_t B, int64_t rows, void* base) {
-  const SeqTiling t = tiling(c, B, rows);
+static size_t carve(SeqParams& p, const Ctx* c, int32_t B, int64_t rows, bool alone, void* base) {
+  const SeqTiling t = tiling(c, B, rows, alone);
   p.tok = t.tok; p.kt = t.kt; p.chunk_min = t.chunk_min; p.chunk_target = t.chunk_target;
   p.ctas = t.ctas; p.item_cost = t.item_cost; p.split_cost = t.split_cost;
   const int64_t R = (int64_t)t.tok * p.G, pieces = 2ll * t.chunk_target / p.Hkv;
@@ -84,8 +106,9 @@ static SeqParams shape(const Ctx* c) {
 }
 
 static lime_status attend(const Ctx* c, SeqParams& p, bool tree, void* ws, size_t ws_bytes, cudaStream_t st) {
+  const bool alone = tree && p.k == nullptr;
   char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
-  const size_t need = carve(p, c, p.B, p.q_rows, base);
+  const size_t need = carve(p, c, p.B, p.q_rows, alone, base);
   if (ws == nullptr || ws_bytes < need + (size_t)(base - static_cast<char*>(ws))) return LIME_WORKSPACE_TOO_SMALL;
   // what the host knows of the keys bounds the pieces as well
   const int64_t most = tree ? (int64_t)p.max_pages * p.page_rows + (p.k ? p.q_rows + p.kt : 0) : p.kv_rows;
@@ -96,7 +119,9 @@ static lime_status attend(const Ctx* c, SeqParams& p, bool tree, void* ws, size_
   if ((int64_t)p.items_upper * p.Hkv > kMaxRows) return LIME_UNSUPPORTED_SHAPE;      // (a round of CTAs past the last item stays inside 32 bits)
   lime_status s;
   if ((s = launch_seq_schedule(p, tree, st)) != LIME_OK) return s;
-  s = c->cfg.dtype == LIME_BF16 ? (p.dh <= 64 ? launch_seq_attn_d64_tc(p, tree, st) : launch_seq_attn_tc(p, tree, st)) : launch_seq_attn_simt(p, tree, tiling(c, p.B, p.q_rows).few, st);
+  if (c->cfg.dtype != LIME_BF16) s = launch_seq_attn_simt(p, tree, tiling(c, p.B, p.q_rows, alone).few, st);
+  else if (streams(c, p.B, p.q_rows, alone)) s = launch_seq_attn_few(p, st);
+  else s = p.dh <= 64 ? launch_seq_attn_d64_tc(p, tree, st) : launch_seq_attn_tc(p, tree, st);
   if (s != LIME_OK) return s;
   return may_split ? launch_seq_merge(p, c->cfg.dtype, st) : LIME_OK;
 }
@@ -158,7 +183,8 @@ size_t lime_sequence_workspace_bytes(const lime_ctx* ctx, int32_t B, int64_t row
   const Ctx* c = reinterpret_cast<const Ctx*>(ctx);
   if (!c->have_seq) return 0;
   SeqParams p = shape(c);
-  return carve(p, c, B, rows, nullptr) + 256;
+  const size_t any = carve(p, c, B, rows, false, nullptr), alone = carve(p, c, B, rows, true, nullptr);
+  return (any > alone ? any : alone) + 256;
 }
 
 lime_status lime_attend_history(lime_ctx* ctx, const void* q, int64_t q_stride, const int32_t* off, const void* k, int64_t k_stride,

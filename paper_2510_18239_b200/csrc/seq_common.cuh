@@ -23,7 +23,7 @@ struct SeqItem {
   int32_t part;           // where the partial result goes; -1: the item is the whole row tile
 };
 struct SeqSplit { int32_t row0, rows, part0, n; };       // a row tile cut into n items, parts part0 ..
-struct SeqPlan { int32_t n_items, n_split, n_parts, pad; };
+struct SeqPlan { int32_t n_items, n_split; };
 
 struct SeqParams {
   const void *q, *k, *v;                 // history: k, v the packed keys; tree: the new rows' (nullable)
@@ -105,6 +105,7 @@ lime_status launch_seq_schedule(const SeqParams& p, bool tree, cudaStream_t st);
 lime_status launch_seq_merge(const SeqParams& p, int dtype, cudaStream_t st);
 lime_status launch_seq_attn_tc(const SeqParams& p, bool tree, cudaStream_t st);        // bf16, d_h > 64
 lime_status launch_seq_attn_d64_tc(const SeqParams& p, bool tree, cudaStream_t st);    // bf16, d_h <= 64
-lime_status launch_seq_attn_simt(const SeqParams& p, bool tree, bool few_rows, cudaStream_t st);                    // fp32
+lime_status launch_seq_attn_few(const SeqParams& p, cudaStream_t st);                   // bf16, up to 8 stacked rows, the cache alone
+lime_status launch_seq_attn_simt(const SeqParams& p, bool tree, bool few_rows, cudaStream_t st);  // fp32
 
 }  // namespace lime

@@ -379,6 +379,64 @@ def test_many_users_and_offsets_past_the_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_offsets_past_32_bits(dtype):
+    """Rows 2^20 elements apart, the last ones more than 2^31 elements in; a cache of more than 2^31 elements, used at its end."""
+    gen = torch.Generator().manual_seed(37)
+    Hq, Hkv, dh, rows, n = 4, 2, 64, 2200, 130
+    m = lime(dtype, Hq, Hkv, dh, rot_dim=64)
+    wide = torch.empty(rows, 1 << 20, dtype=TYPES[dtype], device="cuda")
+    part = lambda at, h: wide[:, at:at + h * dh].unflatten(1, (h, dh))
+    q, k, v, out = part(0, Hq), part(512, Hkv), part(1024, Hkv), part(4096, Hq)
+    qkv = [rand(gen, rows, h, dh, dtype=dtype) for h in (Hq, Hkv, Hkv)]
+    for to, x in zip((q, k, v), qkv):
+        to.copy_(x)
+    off = torch.tensor([0, rows - n, rows], dtype=torch.int32).cuda()
+    out.fill_(7)
+    m.attend_history(q, k, v, off, out=out)
+    ref, mag, size = so.attend(*(f64(x[-n:]) for x in qkv), so.causal(n, n), 1 / 8)
+    close(out[-n:], ref, mag, size, dh, n, dtype)
+    # into the last pages of a cache, and from there; the rest of the last but one is whatever the memory held
+    page, n_pages = 128, 131200
+    ck = torch.empty(n_pages, page, Hkv, dh, dtype=TYPES[dtype], device="cuda")
+    cv = torch.empty_like(ck)
+    slots = torch.full((rows,), -1, dtype=torch.int32)
+    slots[-n:-2] = (n_pages - 1) * page + torch.arange(page, dtype=torch.int32)
+    slots[-2:] = (n_pages - 2) * page + torch.arange(2, dtype=torch.int32)
+    pos = torch.arange(rows, dtype=torch.int32)
+    m.norm_rotate(q, k, pos.cuda(), v=v, q_out=q, k_out=k, cache_k=ck, cache_v=cv, slots=slots.cuda())
+    close_rotated(q[-n:], f64(qkv[0][-n:]), None, pos[-n:].numpy(), 64, False, 10000.0, 1e-6, dtype)
+    assert torch.equal(ck[-1], k[-n:-2]) and torch.equal(cv[-2, :2], v[-2:])
+    table = torch.tensor([[n_pages - 1, n_pages - 2]], dtype=torch.int32).cuda()
+    got = m.attend_tree(q[-3:], ck, cv, table, torch.tensor([n], dtype=torch.int32).cuda(), off_of([3]))
+    ref, mag, size = so.attend(f64(q[-3:]), f64(k[-n:]), f64(v[-n:]), np.ones((3, n), bool), 1 / 8)
+    close(got, ref, mag, size, dh, n, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hq,Hkv,dh", [(1024, 1024, 8), (1024, 16, 128), (1024, 512, 64), (64, 1, 8)])
+def test_the_most_heads(dtype, Hq, Hkv, dh):
+    gen = torch.Generator().manual_seed(Hkv)
+    m = lime(dtype, Hq, Hkv, dh, rot_dim=dh)
+    check_history(m, gen, dtype, Hq, Hkv, dh, [3, 0, 1], [3, 5, 70], 1 / np.sqrt(dh), tail=1)
+    check_tree(m, gen, dtype, Hq, Hkv, dh, [1, 3], [20, 0], 16, "drafts")
+    q, k, gamma = rand(gen, 5, Hq, dh, dtype=dtype), rand(gen, 5, Hkv, dh, dtype=dtype), rand(gen, dh, dtype=dtype)
+    pos = torch.tensor([0, 1, 7, 100, 5000], dtype=torch.int32)
+    oq, ok = m.norm_rotate(q.cuda(), k.cuda(), pos.cuda(), gamma_q=gamma.cuda(), gamma_k=gamma.cuda())
+    close_rotated(oq, f64(q), f64(gamma), pos.numpy(), dh, False, 10000.0, 1e-6, dtype)
+    close_rotated(ok, f64(k), f64(gamma), pos.numpy(), dh, False, 10000.0, 1e-6, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+def test_the_largest_pages_and_long_trees(dtype, dh):
+    gen = torch.Generator().manual_seed(dh)
+    m = lime(dtype, 2, 1, dh)
+    check_tree(m, gen, dtype, 2, 1, dh, [2, 1], [5000, 4096], 4096, "drafts")
+    check_tree(m, gen, dtype, 2, 1, dh, [700, 9], [65, 1], 32, "roots")
+    check_tree(m, gen, dtype, 2, 1, dh, [900], [33], 16, "drafts", parent=torch.arange(900, dtype=torch.int32) - 1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_a_graph_serves_other_lengths_than_it_was_captured_with(dtype):
     """Lengths, tables and trees are device data: a replay reads what stands there then."""
     gen = torch.Generator().manual_seed(53)
