@@ -97,7 +97,8 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
   uint64_t* kv_full = bars;            // [5]  keys or values of a tile landed
   uint64_t* kv_empty = bars + 10;      // [5]  every MMA that reads them has run
-  uint64_t* mend_done = bars + 20;     // [5]  the value tile in this stage is mended
+  uint64_t* mend_ask = bars + 20;      //      the next value tile to be mended is on its way
+  uint64_t* mend_done = bars + 21;     //      it is mended
   uint64_t* q_full = bars + 30;        //      queries of an item landed
   uint64_t* q_empty = bars + 32;       //      every score MMA that reads them has run
   uint64_t* s_full = bars + 34;        // [2]  scores of the slot in TMEM
@@ -114,7 +115,8 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < STAGES; ++i) { mbar_init(&kv_full[i], 1); mbar_init(&kv_empty[i], 1); mbar_init(&mend_done[i], 1); }
+    for (int i = 0; i < STAGES; ++i) { mbar_init(&kv_full[i], 1); mbar_init(&kv_empty[i], 1); }
+    mbar_init(mend_ask, 1); mbar_init(mend_done, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&s_free[i], 1); mbar_init(&pv_done[i], 1);
       mbar_init(&p_ready[i], 4); mbar_init(&o_free[i], 4); mbar_init(&x_free[i], 4); mbar_init(&ml_full[i], 4);
@@ -142,7 +144,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     bool ok = true;
     int g = 0, qn = 0;                                       // tiles of keys and values so far (ring position); items with key tiles
     uint32_t ph0 = 0, ph1 = 0;                               // phases of the slots' barriers that this role waits for
-    uint32_t mend_ph = 0;                                    // a bit for every stage
+    uint32_t mend_ph = 0;
     bool prev = false, prev_same = false;                    // an item before this one, and its slots were joined
     uint32_t o_ph = 0, x_ph = 0;                             // phases in which that item's accumulators are read out
     for (int pass = 0; pass < 2; ++pass) {
@@ -239,14 +241,21 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           auto taken = [&](int s) {
             return !prev || __all_sync(0xffffffffu, mbar_wait(&o_free[s], o_ph, p.err, 124) && (!prev_same || mbar_wait(&x_free[s], x_ph, p.err, 125)));
           };
+          // a tile is asked for one ahead, when the stage's load before this one has landed and the mending before it is done
+          auto ask = [&](int t) {
+            if ((TREE || again) && t < w.it.t1 && w.mended(seq_tile<TREE>(p, w.it, w.n_tree, t), again) && lane == 0) mbar_arrive(mend_ask);
+            __syncwarp();
+          };
+          ask(w.it.t0);
           for (int t = w.it.t0; t < w.it.t1 && ok; ++t, g += 2) {
             const int st = (g + 1) % STAGES;
             const SeqTile k = seq_tile<TREE>(p, w.it, w.n_tree, t);
             if (!__all_sync(0xffffffffu, mbar_wait(&kv_full[st], (uint32_t)((g + 1) / STAGES) & 1u, p.err, 115))) { ok = false; break; }
             if (w.mended(k, again)) {
-              if (!__all_sync(0xffffffffu, mbar_wait(&mend_done[st], (mend_ph >> st) & 1u, p.err, 116))) { ok = false; break; }
-              mend_ph ^= 1u << st;
+              if (!__all_sync(0xffffffffu, mbar_wait(mend_done, mend_ph, p.err, 116))) { ok = false; break; }
+              mend_ph ^= 1u;
             }
+            ask(t + 1);
             const uint64_t dv = dv0 + (uint64_t)((uint32_t)st * C::TILE >> 4);
             for (int s = 0; s < 2; ++s) {
               if (!w.takes(s, t)) continue;
@@ -278,15 +287,16 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           prev_same = w.same;
         } else {
           // ---------------------------------------------------------------- value tiles that need mending
-          // Every load is waited for, so that a stage's phase is never taken for the one two before it (without a cache nothing is mended
-          // in the first pass, and all of its loads have landed before the second).
+          // Asked for one at a time by the warp that will use it: the ring waits for that warp and not for this one, which could
+          // otherwise fall a round behind and take a stage's phase for the one two before it.
           for (int t = w.it.t0; t < w.it.t1 && ok; ++t, g += 2) {
             if (!TREE && !again) continue;
             const SeqTile k = seq_tile<TREE>(p, w.it, w.n_tree, t);
-            const int st = (g + 1) % STAGES;
-            if (!__all_sync(0xffffffffu, mbar_wait(&kv_full[g % STAGES], (uint32_t)(g / STAGES) & 1u, p.err, 119) &&
-                                             mbar_wait(&kv_full[st], (uint32_t)((g + 1) / STAGES) & 1u, p.err, 118))) { ok = false; break; }
             if (!w.mended(k, again)) continue;
+            const int st = (g + 1) % STAGES;
+            if (!__all_sync(0xffffffffu, mbar_wait(mend_ask, mend_ph, p.err, 119) &&
+                                             mbar_wait(&kv_full[st], (uint32_t)((g + 1) / STAGES) & 1u, p.err, 118))) { ok = false; break; }
+            mend_ph ^= 1u;
             uint8_t* tile = smem + C::OFF_KV + st * C::TILE;
             const int n = k.n - k.j0;                        // rows of the tile that there are
             for (int i = lane; i < 128 * (DHP / 64) * 8; i += 32) {
@@ -301,7 +311,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             }
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&mend_done[st]);
+            if (lane == 0) mbar_arrive(mend_done);
           }
         }
       }
@@ -362,6 +372,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 for (int i = 0; i < 4; ++i) see[i] |= (b >> 5) == i ? 1u << (b & 31) : 0u;
                 anc = seq_parent(p, first_row, anc);
               }
+              __syncwarp();                                // (tensor memory is read and written by whole warps)
 #pragma unroll
               for (int j = 0; j < 128; ++j)
                 if (((see[j >> 5] >> (j & 31)) & 1u) == 0) v[j] = -INFINITY;

@@ -3,12 +3,6 @@
 
 #include "seq_common.cuh"
 #include "tc_common.cuh"
-#ifndef FEW_MIN
-#define FEW_MIN 4
-#define FEW_TGT 4
-#define FEW_ITEM 4.f
-#define FEW_SPLIT 2.f
-#endif
 
 namespace lime {
 
@@ -26,13 +20,21 @@ static lime_status ready(const Ctx* c) {
 }
 constexpr int64_t kMaxRows = 0x7fff0000LL;       // row indexes and the ends of the tiles that hold them stay inside 32 bits
 
-// How the rows of a batch are tiled, and how fine a batch may be cut (both attention calls).
-struct SeqTiling { int tok, kt, chunk_min, chunk_target, ctas; float item_cost, split_cost; bool few; };
-// `alone`: nothing but the cache is attended to.
+// Whether the rows go to k_seq_attn_few: up to 8 stacked rows a user on average that attend to nothing but the cache (`alone`).  On the
+// tensor cores' tiles of 128 rows instead: 64 events of 16 heads over 4 heads of 128 221 against 180 us, 256 of 4 over 4 of 32 53 against
+// 24.5, one of 8 over 2 of 64 17 against 11.6.
 static bool streams(const Ctx* c, int32_t B, int64_t rows, bool alone) {
   const int G = c->seq.Hq / c->seq.Hkv;
   return alone && c->cfg.dtype == LIME_BF16 && G <= 8 && rows * G <= 8ll * B;
 }
+// How the rows of a batch are tiled, and how fine a batch may be cut (both attention calls).  Pieces are worth a merge where there are
+// few of them or little to merge; the figures are in us, the other choice first.
+//   streamed rows: pieces of 4 tiles and more (2: 8 events over 500..5000 rows 25.6, now 18.0; 8: one event over 1000 14.0, 12.3), four a
+//     CTA (2: 64 events over 16..16384 235, 217; 8: 232);
+//   tensor cores: FEWNOTE
+//   CUDA cores, d_h = 64: 16 stacked rows a tile where a user has no more on average (64: 64 events of 8 heads over 100..3000 rows 148,
+//     100; three rows over 2000 36.9, 27.6).
+struct SeqTiling { int tok, kt, chunk_min, chunk_target, ctas; float item_cost, split_cost; bool few; };
 static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows, bool alone) {
   const int G = c->seq.Hq / c->seq.Hkv;
   SeqTiling t;
@@ -40,11 +42,11 @@ static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows, bool alone) {
     t.few = true;
     t.tok = 8 / G;
     t.kt = 64;
-    t.ctas = (c->seq.d_h <= 64 ? 4 : 3) * kSMs;
-    t.chunk_min = FEW_MIN;
-    t.chunk_target = FEW_TGT * t.ctas;
-    t.item_cost = FEW_ITEM;
-    t.split_cost = FEW_SPLIT;
+    t.ctas = seq_few_blocks(c->seq.d_h) * kSMs;
+    t.chunk_min = 4;
+    t.chunk_target = 4 * t.ctas;
+    t.item_cost = 4.f;
+    t.split_cost = 2.f;
     return t;
   }
   if (c->cfg.dtype == LIME_BF16) {

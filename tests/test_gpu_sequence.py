@@ -436,6 +436,43 @@ def test_the_largest_pages_and_long_trees(dtype, dh):
     check_tree(m, gen, dtype, 2, 1, dh, [900], [33], 16, "drafts", parent=torch.arange(900, dtype=torch.int32) - 1)
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh", [("f32", 8, 2, 64), ("bf16", 4, 4, 32), ("bf16", 8, 2, 64), ("bf16", 16, 4, 128)])
+@pytest.mark.parametrize("form", ["history", "none", "roots", "drafts"])
+def test_many_calls_in_a_row_give_the_same(dtype, Hq, Hkv, dh, form):
+    """Calls overlap at their ends; their warps wait for one another in orders that differ from call to call.  Every result is the first
+    one's, and no bounded wait runs out."""
+    gen = torch.Generator().manual_seed(dh)
+    m = lime(dtype, Hq, Hkv, dh)
+    B, page = 48, 64
+    n, c = [4] * B, [16 + 3000 * b // B for b in range(B)]
+    q, k, v = (rand(gen, 4 * B, h, dh, dtype=dtype).cuda() for h in (Hq, Hkv, Hkv))
+    if form == "history":
+        keys = [a // 8 + 4 for a in c]
+        k, v = (rand(gen, sum(keys), Hkv, dh, dtype=dtype).cuda() for _ in range(2))
+        off, kv_off = off_of(n), off_of(keys)
+        call = lambda out: m.attend_history(q, k, v, off, kv_off=kv_off, out=out)
+    else:
+        ck, cv, table = paged(gen, c, page, Hkv, dh, dtype)
+        ck, cv, table, ctx = ck.cuda(), cv.cuda(), table.cuda(), torch.tensor(c, dtype=torch.int32).cuda()
+        rows = B if form == "none" else 4 * B
+        off = off_of([rows // B] * B)
+        new = {} if form == "none" else dict(tree_k=k, tree_v=v)
+        if form == "drafts":
+            new["parent"] = torch.tensor([-1, 0, 0, 1] * B, dtype=torch.int32).cuda()
+        q = q[:rows]
+        call = lambda out: m.attend_tree(q, ck, cv, table, ctx, off, out=out, **new)
+    first = call(torch.empty_like(q))
+    outs = [torch.empty_like(q) for _ in range(25)]
+    differ = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(40):
+        for o in outs:
+            call(o)
+        for o in outs:
+            differ += (o != first).sum()
+    assert int(differ) == 0
+    binding.lime_device_status(m.ctx)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_a_graph_serves_other_lengths_than_it_was_captured_with(dtype):
     """Lengths, tables and trees are device data: a replay reads what stands there then."""
