@@ -31,7 +31,8 @@ static bool streams(const Ctx* c, int32_t B, int64_t rows, bool alone) {
 // few of them or little to merge; the figures are in us, the other choice first.
 //   streamed rows: pieces of 4 tiles and more (2: 8 events over 500..5000 rows 25.6, now 18.0; 8: one event over 1000 14.0, 12.3), four a
 //     CTA (2: 64 events over 16..16384 235, 217; 8: 232);
-//   tensor cores: FEWNOTE
+//   tensor cores: of 8 tiles and more, which cost a merge as much as 8 more (4 and 1: 64 events behind 16..8000 rows, 16 heads over 4 of 128
+//     119, 108; 2 and 1: 8 events of 16 heads over one of 64 41.2, 26.7; but a draft of 5 over 1000 rows 20.8, 21.9);
 //   CUDA cores, d_h = 64: 16 stacked rows a tile where a user has no more on average (64: 64 events of 8 heads over 100..3000 rows 148,
 //     100; three rows over 2000 36.9, 27.6).
 struct SeqTiling { int tok, kt, chunk_min, chunk_target, ctas; float item_cost, split_cost; bool few; };
@@ -52,14 +53,14 @@ static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows, bool alone) {
   if (c->cfg.dtype == LIME_BF16) {
     // tensor cores: 128 stacked rows a CTA and two CTAs an SM, or two slots of 128 rows
     const bool narrow = c->seq.d_h <= 64;
-    t.few = rows * G <= 64ll * B;                   // partial results of a few rows cost little
+    t.few = false;
     t.tok = (narrow ? 1 : 2) * (128 / G);
     t.kt = narrow ? 64 : 128;
     t.ctas = (narrow ? 2 : 1) * kSMs;
-    t.chunk_min = t.few ? (narrow ? 2 : 4) : 8;
-    t.chunk_target = (t.few ? 8 : 4) * t.ctas;
+    t.chunk_min = 8;
+    t.chunk_target = 4 * t.ctas;
     t.item_cost = narrow ? 4.f : 6.f;
-    t.split_cost = t.few ? 1.f : 8.f;
+    t.split_cost = 8.f;
     return t;
   }
   // CUDA cores: 64 stacked rows a tile, or 16 where a user has no more on average
