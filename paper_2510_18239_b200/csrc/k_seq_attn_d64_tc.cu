@@ -46,7 +46,7 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   uint64_t* s_full = bars + 18;        //     scores in TMEM
   uint64_t* p_ready = bars + 19;       //     probabilities in TMEM (four warps)
   uint64_t* pv_done = bars + 20;       //     their values are in the accumulator
-  uint64_t* o_free = bars + 21;        //     the accumulator of an item is read out (four warps)
+  uint64_t* o_free = bars + 21;        //     the accumulator of an item with key tiles is read out (four warps)
   uint64_t* s_free = bars + 22;        //     the scores of a tile are in registers (four warps; OWN_P)
   int* s_flags = reinterpret_cast<int*>(bars + 23);         // 1: some result is not finite, 2: a wait gave up
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_flags + 1);
@@ -86,17 +86,15 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       for (SeqWalk at(p, s_bad, pass > 0); ok && at.work >= 0; at.next(p, s_bad, pass > 0)) {
         const SeqItem it = seq_item(p, at.work);
         const int kvh = at.work % p.Hkv, n_tree = TREE ? seq_tree_tiles(p, it) : 0;
-        const bool any = it.t0 < it.t1;
+        if (it.t0 >= it.t1) continue;                        // nothing to see: its rows are zeros, without any of this
         // ------------------------------------------------------------------ loads
-        if (any) {
-          if (!__all_sync(0xffffffffu, mbar_wait(q_empty, ((uint32_t)qn & 1u) ^ 1u, p.err, 141))) { ok = false; break; }
-          if (lane == 0) {
-            mbar_arrive_expect_tx(q_full, (uint32_t)(p.tok * G) * 128u);
-            tma_load_3d(smem, &tmQ, 0, kvh * G, it.row0, q_full);
-          }
-          __syncwarp();
-          ++qn;
+        if (!__all_sync(0xffffffffu, mbar_wait(q_empty, ((uint32_t)qn & 1u) ^ 1u, p.err, 141))) { ok = false; break; }
+        if (lane == 0) {
+          mbar_arrive_expect_tx(q_full, (uint32_t)(p.tok * G) * 128u);
+          tma_load_3d(smem, &tmQ, 0, kvh * G, it.row0, q_full);
         }
+        __syncwarp();
+        ++qn;
         const int box = min(p.page_rows, KEYS);              // rows of a page in one copy
         int row = 0;                                         // of the lane's page of the coming tile of cached rows
         auto look_up = [&](int t) {
@@ -140,13 +138,13 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   } else if (warp == 1) {
     bool ok = true;
     int g = 0, qn = 0;
-    uint32_t n = 0, done = 0;                                // tiles so far; items so far
+    uint32_t n = 0, done = 0;                                // tiles so far; items with tiles so far
     for (int pass = 0; pass < 2; ++pass) {
       const bool again = pass > 0;
       for (SeqWalk at(p, s_bad, again); ok && at.work >= 0; at.next(p, s_bad, again)) {
         const SeqItem it = seq_item(p, at.work);
         const int n_tree = TREE ? seq_tree_tiles(p, it) : 0;
-        const bool any = it.t0 < it.t1;
+        if (it.t0 >= it.t1) continue;
         // ------------------------------------------------------------------ both products: values of a tile, then scores of the next
         const uint32_t tmem_u = __shfl_sync(0xffffffffu, tmem_base, 0), idesc_s = make_idesc_bf16(128, KEYS), idesc_o = make_idesc_bf16(128, ksteps * 16, false, true);
         const uint64_t dq = make_sdesc_k_sw128(smem_u32(smem)), dk0 = make_sdesc_k_sw128(smem_u32(smem) + kD64OffKv), dv0 = make_sdesc_mn_sw128(smem_u32(smem) + kD64OffKv, kD64Tile);
@@ -169,16 +167,11 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           __syncwarp();
           return true;
         };
-        // the accumulator as the item before left it is read out (waited for without key tiles too, so that no phase is missed)
+        // the accumulator as the item before left it is read out
         auto taken = [&] { return done == 0 || __all_sync(0xffffffffu, mbar_wait(o_free, (done - 1) & 1u, p.err, 146)); };
-        if (any) {
-          if (!__all_sync(0xffffffffu, mbar_wait(q_full, (uint32_t)qn & 1u, p.err, 144))) { ok = false; break; }
-          ++qn;
-          if (!scores(it.t0)) { ok = false; break; }
-        } else if (!taken()) {
-          ok = false;
-          break;
-        }
+        if (!__all_sync(0xffffffffu, mbar_wait(q_full, (uint32_t)qn & 1u, p.err, 144))) { ok = false; break; }
+        ++qn;
+        if (!scores(it.t0)) { ok = false; break; }
         for (int t = it.t0; t < it.t1; ++t, ++n) {
           if (OWN_P && !(__all_sync(0xffffffffu, mbar_wait(s_free, n & 1u, p.err, 151)) && (t + 1 >= it.t1 || scores(t + 1)))) { ok = false; break; }
           g = k0 + 2 * (t - it.t0) + 1;                      // its values
@@ -209,7 +202,7 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           __syncwarp();
           if (!OWN_P && t + 1 < it.t1 && !scores(t + 1)) { ok = false; break; }
         }
-        if (any) ++g;
+        ++g;
         ++done;
       }
       if (end_of_pass(ok) != 1) break;
@@ -377,7 +370,7 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(o_free);
+        if (any && lane == 0) mbar_arrive(o_free);
       }
       if (end_of_pass(ok) != 1) break;
     }

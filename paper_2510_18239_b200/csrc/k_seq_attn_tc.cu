@@ -9,7 +9,7 @@
 //   O [128 x d_h]     += P [128 x 128] . V_tile        P as bf16 in tensor memory, over its own scores; V as it lies (MN-major)
 // Two slots because one alone is a chain (scores, softmax, values) several times its tensor time: while the softmax warps of one work,
 // the pipe works for the other.  An item of no more than 128 rows puts the same rows into both slots, which take the key tiles in turn
-// and are joined in the end; so a single new event streams its cache through two chains.
+// and are joined in the end; so a few new rows stream their cache through two chains.
 //  * Warp 0 loads (one lane a page where keys lie in pages), warp 1 issues the scores, warp 2 the values, warp 3 mends value tiles (below);
 //    warps 4..7 and 8..11 are the softmax of a slot, one thread per row.  Online softmax with lazy rescale: the reference maximum is
 //    raised only when exceeded by 2^8.
@@ -29,7 +29,7 @@
 // of the tiles before, without waiting for the maximum (1.15 ms); 64-key tiles with two score buffers a slot, which take the scores out of
 // the chain (1.24 ms); two threads a row, 16 softmax warps (1.18 ms); the first half of the probabilities handed over early, polling
 // without a pause (no change).
-// Single events stream their keys at 0.70 of the copy rate (64 users of 16..16384 keys, 1.07 GB: 231 us).
+// A few rows stream their keys at 0.70 of the copy rate (64 users' 4 drafts over 16..16384 rows, 1.07 GB: 234 us).
 #include "seq_tc.cuh"
 
 namespace lime {
@@ -105,10 +105,12 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   uint64_t* s_free = bars + 36;        // [2]  the values of the slot's last probabilities are issued: new scores may follow in the pipe
   uint64_t* p_ready = bars + 38;       // [2]  probabilities in TMEM (four warps)
   uint64_t* pv_done = bars + 40;       // [2]  the slot's accumulator is up to date
-  uint64_t* o_free = bars + 42;        // [2]  the slot's accumulator is read out, by its own warps (every item)
+  // (of items that have key tiles; the first two of those in which the slot has one, so that none runs ahead of the values by two phases)
+  uint64_t* o_free = bars + 42;        // [2]  the slot's accumulator is read out, by its own warps
   uint64_t* x_free = bars + 44;        // [2]  and by the other slot's (items whose slots are joined)
   uint64_t* ml_full = bars + 46;       // [2]  the slot's references and sums are in shared memory (items whose slots are joined)
-  int* s_flags = reinterpret_cast<int*>(bars + 48);         // 1: some result is not finite, 2: a wait gave up
+  uint64_t* ml_free = bars + 48;       // [2]  and read by the other slot
+  int* s_flags = reinterpret_cast<int*>(bars + 50);         // 1: some result is not finite, 2: a wait gave up
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_flags + 1);
   float2* s_ml = reinterpret_cast<float2*>(smem + C::OFF_ML);
   uint32_t* s_bad = reinterpret_cast<uint32_t*>(smem + C::OFF_BAD);
@@ -119,7 +121,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     mbar_init(mend_ask, 1); mbar_init(mend_done, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&s_free[i], 1); mbar_init(&pv_done[i], 1);
-      mbar_init(&p_ready[i], 4); mbar_init(&o_free[i], 4); mbar_init(&x_free[i], 4); mbar_init(&ml_full[i], 4);
+      mbar_init(&p_ready[i], 4); mbar_init(&o_free[i], 4); mbar_init(&x_free[i], 4); mbar_init(&ml_full[i], 4); mbar_init(&ml_free[i], 4);
     }
     *s_flags = 0;
     fence_barrier_init();
@@ -145,28 +147,26 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     int g = 0, qn = 0;                                       // tiles of keys and values so far (ring position); items with key tiles
     uint32_t ph0 = 0, ph1 = 0;                               // phases of the slots' barriers that this role waits for
     uint32_t mend_ph = 0;
-    bool prev = false, prev_same = false;                    // an item before this one, and its slots were joined
-    uint32_t o_ph = 0, x_ph = 0;                             // phases in which that item's accumulators are read out
+    // values: a bit for every slot whose accumulator an item before left to be read out, by its own warps and by the other slot's; phases
+    uint32_t own_out = 0, cross_out = 0, o_ph = 0, x_ph = 0;
     for (int pass = 0; pass < 2; ++pass) {
       const bool again = pass > 0;
       for (SeqWalk at(p, s_bad, again); ok && at.work >= 0; at.next(p, s_bad, again)) {
         const int kvh = at.work % p.Hkv;
         const SeqWork<TREE> w(p, at.work);
-        const bool any = w.it.t0 < w.it.t1;
+        if (w.it.t0 >= w.it.t1) continue;                    // nothing to see: its rows are zeros, without any of this
         const uint32_t q_ph = (uint32_t)qn & 1u;
-        if (any) ++qn;
+        ++qn;
         if (warp == 0) {
           // ---------------------------------------------------------------- loads
-          if (any) {
-            if (!__all_sync(0xffffffffu, mbar_wait(q_empty, q_ph ^ 1u, p.err, 123))) { ok = false; break; }
-            if (lane == 0) {
-              mbar_arrive_expect_tx(q_full, (w.same ? 1u : 2u) * (uint32_t)(w.ts * G) * 128u * (DHP / 64));
-              for (int s = 0; s < (w.same ? 1 : 2); ++s)
-                for (int c = 0; c < DHP / 64; ++c)
-                  tma_load_3d(smem + C::OFF_Q + s * C::TILE + c * C::SUB, &tmQ, c * 64, kvh * G, w.it.row0 + s * w.ts, q_full);
-            }
-            __syncwarp();
+          if (!__all_sync(0xffffffffu, mbar_wait(q_empty, q_ph ^ 1u, p.err, 123))) { ok = false; break; }
+          if (lane == 0) {
+            mbar_arrive_expect_tx(q_full, (w.same ? 1u : 2u) * (uint32_t)(w.ts * G) * 128u * (DHP / 64));
+            for (int s = 0; s < (w.same ? 1 : 2); ++s)
+              for (int c = 0; c < DHP / 64; ++c)
+                tma_load_3d(smem + C::OFF_Q + s * C::TILE + c * C::SUB, &tmQ, c * 64, kvh * G, w.it.row0 + s * w.ts, q_full);
           }
+          __syncwarp();
           const int box = min(p.page_rows, 128);             // rows of a page in one copy
           int row = 0;                                       // of the lane's page of the coming tile of cached rows
           auto look_up = [&](int t) {
@@ -205,7 +205,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           // ---------------------------------------------------------------- scores
           const uint32_t idesc = make_idesc_bf16(128, 128);
           const uint64_t dq0 = make_sdesc_k_sw128(smem_u32(smem) + C::OFF_Q), dk0 = make_sdesc_k_sw128(smem_u32(smem) + C::OFF_KV);
-          if (any && !__all_sync(0xffffffffu, mbar_wait(q_full, q_ph, p.err, 112))) { ok = false; break; }
+          if (!__all_sync(0xffffffffu, mbar_wait(q_full, q_ph, p.err, 112))) { ok = false; break; }
           for (int t = w.it.t0; t < w.it.t1 && ok; ++t, g += 2) {
             const int st = g % STAGES;
             if (!__all_sync(0xffffffffu, mbar_wait(&kv_full[st], (uint32_t)(g / STAGES) & 1u, p.err, 113))) { ok = false; break; }
@@ -237,9 +237,16 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           const uint32_t idesc = make_idesc_bf16(128, ksteps * 16, false, true);
           const uint64_t dv0 = make_sdesc_mn_sw128(smem_u32(smem) + C::OFF_KV, C::SUB);
           bool first0 = true, first1 = true;
-          // the accumulator of slot s as the item before left it is read out
+          // the accumulator of slot s as an item before left it is read out
           auto taken = [&](int s) {
-            return !prev || __all_sync(0xffffffffu, mbar_wait(&o_free[s], o_ph, p.err, 124) && (!prev_same || mbar_wait(&x_free[s], x_ph, p.err, 125)));
+            const uint32_t bit = 1u << s;
+            const bool done = (!(own_out & bit) || mbar_wait(&o_free[s], (o_ph >> s) & 1u, p.err, 124)) &&
+                              (!(cross_out & bit) || mbar_wait(&x_free[s], (x_ph >> s) & 1u, p.err, 125));
+            o_ph ^= own_out & bit;
+            x_ph ^= cross_out & bit;
+            own_out |= bit;
+            cross_out = w.same ? cross_out | bit : cross_out & ~bit;
+            return __all_sync(0xffffffffu, done);
           };
           // a tile is asked for one ahead, when the stage's load before this one has landed and the mending before it is done
           auto ask = [&](int t) {
@@ -280,11 +287,6 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             if (ok && elect_one()) mma_commit(&kv_empty[st]);
             __syncwarp();
           }
-          // every phase of these barriers is waited for, so that none is taken for the one two before it
-          if (ok && ((first0 && !taken(0)) || (first1 && !taken(1)))) ok = false;
-          if (prev) { o_ph ^= 1u; if (prev_same) x_ph ^= 1u; }
-          prev = true;
-          prev_same = w.same;
         } else {
           // ---------------------------------------------------------------- value tiles that need mending
           // Asked for one at a time by the warp that will use it: the ring waits for that warp and not for this one, which could
@@ -441,9 +443,8 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         // ------------------------------------------------------------------ result: the slot's rows, or of joined slots half the columns
         float w0 = 1.f, w1 = 0.f;                            // of this slot's accumulator and the other's
         const bool have0 = mine, have1 = w.same && w.it.t1 - w.it.t0 > (s ^ 1);
-        if (w.same) {
-          // (read for the joined item before this one: its value contractions were behind that, but this slot may have had no tile)
-          if (joined > 0 && !__all_sync(0xffffffffu, mbar_wait(&x_free[s], (joined - 1) & 1u, p.err, 127))) { ok = false; break; }
+        if (w.same && w.it.t0 < w.it.t1) {
+          if (joined > 0 && !__all_sync(0xffffffffu, mbar_wait(&ml_free[s], (joined - 1) & 1u, p.err, 127))) { ok = false; break; }
           s_ml[s * 128 + r] = make_float2(m, mine ? l : 0.f);
           tc_fence_before();
           __syncwarp();
@@ -451,6 +452,8 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           if (!__all_sync(0xffffffffu, mbar_wait(&ml_full[s ^ 1], joined & 1u, p.err, 126))) { ok = false; break; }
           ++joined;
           const float2 o = s_ml[(s ^ 1) * 128 + r];
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ml_free[s ^ 1]);
           const float mm = fmaxf(m, o.x), ref = mm == -INFINITY ? 0.f : mm;
           w0 = seq_ex2((m - ref) * scale); w1 = seq_ex2((o.x - ref) * scale);
           l = l * w0 + o.y * w1;
@@ -506,8 +509,8 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(&o_free[s]);
-          if (w.same) mbar_arrive(&x_free[s ^ 1]);
+          if (have0) mbar_arrive(&o_free[s]);
+          if (have1) mbar_arrive(&x_free[s ^ 1]);
         }
       }
       if (!ok && lane == 0) atomicOr(s_flags, 2);

@@ -473,6 +473,46 @@ def test_many_calls_in_a_row_give_the_same(dtype, Hq, Hkv, dh, form):
     binding.lime_device_status(m.ctx)
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh", [("f32", 16, 1, 64), ("bf16", 16, 1, 32), ("bf16", 16, 1, 64), ("bf16", 12, 1, 72), ("bf16", 48, 3, 128), ("bf16", 2, 2, 128)])
+def test_runs_of_users_and_rows_that_see_nothing(dtype, Hq, Hkv, dh):
+    """Users without keys, many in a row, between users with one (whose value is the result as it is); queries ahead of the first key.
+    Again and again, as the warps that have nothing to do for them may be far ahead of the others."""
+    gen = torch.Generator().manual_seed(dh + Hq)
+    m = lime(dtype, Hq, Hkv, dh)
+    B = 400
+    has = [int(torch.randint(0, 5, (1,), generator=gen)) == 0 and b > 3 for b in range(B)]
+    n = [1 + b % 9 for b in range(B)]
+    ck, cv, table = paged(gen, [int(h) for h in has], 16, Hkv, dh, dtype)
+    q = rand(gen, sum(n), Hq, dh, dtype=dtype).cuda()
+    args = (ck.cuda(), cv.cuda(), table.cuda(), torch.tensor(has, dtype=torch.int32).cuda(), off_of(n))
+    want = torch.zeros(B, Hkv, dh, dtype=TYPES[dtype])
+    for b in range(B):
+        if has[b]:
+            want[b] = cv[table[b, 0], 0]
+    want = want.repeat_interleave(torch.tensor(n), 0).repeat_interleave(Hq // Hkv, 1).cuda()
+    out = torch.empty_like(q)
+    differ = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(300):
+        differ += (m.attend_tree(q, *args, out=out) != want).sum()
+    # 20 queries a user, the last of which see keys: 0 .. 3 of them
+    nk = [b % 4 if b % 3 else 0 for b in range(B)]
+    q = rand(gen, 20 * B, Hq, dh, dtype=dtype).cuda()
+    k, v = (rand(gen, sum(nk), Hkv, dh, dtype=dtype).cuda() for _ in range(2))
+    off, kv_off = off_of([20] * B), off_of(nk)
+    first, out = m.attend_history(q, k, v, off, kv_off=kv_off), torch.empty_like(q)
+    seen = first.view(B, 20, Hq, dh)
+    j = 0
+    for b, a in enumerate(nk):
+        assert (seen[b, :20 - a] == 0).all()
+        if a:                                                            # the first query that sees a key has that value
+            assert torch.equal(seen[b, 20 - a], v[j].repeat_interleave(Hq // Hkv, 0))
+        j += a
+    for _ in range(300):
+        differ += (m.attend_history(q, k, v, off, kv_off=kv_off, out=out) != first).sum()
+    assert int(differ) == 0
+    binding.lime_device_status(m.ctx)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_a_graph_serves_other_lengths_than_it_was_captured_with(dtype):
     """Lengths, tables and trees are device data: a replay reads what stands there then."""
