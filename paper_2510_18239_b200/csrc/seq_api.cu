@@ -34,7 +34,8 @@ static bool streams(const Ctx* c, int32_t B, int64_t rows, bool alone) {
 //   tensor cores: of 8 tiles and more, which cost a merge as much as 8 more (4 and 1: 64 events behind 16..8000 rows, 16 heads over 4 of 128
 //     119, 108; 2 and 1: 8 events of 16 heads over one of 64 41.2, 26.7; but a draft of 5 over 1000 rows 20.8, 21.9);
 //   CUDA cores, d_h = 64: 16 stacked rows a tile where a user has no more on average (64: 64 events of 8 heads over 100..3000 rows 148,
-//     100; three rows over 2000 36.9, 27.6).
+//     100; three rows over 2000 36.9, 27.6); pieces of 2 tiles and more (4: 7 users' drafts 80.3, 73.8; the events 101, 90; the three rows
+//     27.4, 23.4).
 struct SeqTiling { int tok, kt, chunk_min, chunk_target, ctas; float item_cost, split_cost; bool few; };
 static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows, bool alone) {
   const int G = c->seq.Hq / c->seq.Hkv;
@@ -68,7 +69,7 @@ static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows, bool alone) {
   t.tok = (t.few ? 16 : 64) / G;
   t.kt = 64;
   t.ctas = (c->seq.d_h <= 64 ? 2 : 1) * kSMs;
-  t.chunk_min = 4;
+  t.chunk_min = 2;
   t.chunk_target = 4 * t.ctas;
   t.item_cost = 2.f;
   t.split_cost = 1.f;
