@@ -117,7 +117,9 @@ static lime_status attend(const Ctx* c, SeqParams& p, bool tree, void* ws, size_
   // what the host knows of the keys bounds the pieces as well
   const int64_t most = tree ? (int64_t)p.max_pages * p.page_rows + (p.k ? p.q_rows + p.kt : 0) : p.kv_rows;
   const int64_t tiles = (most + p.kt - 1) / p.kt + 1, pieces = (tiles - 1) / p.chunk_min + 1;
-  const bool may_split = tiles > p.chunk_min;
+  // (with more heads of keys than chunk_target no row tile can be: a chunk is then longer than all of them together, and there is no room
+  // in the list of them)
+  const bool may_split = tiles > p.chunk_min && p.split_upper > 0;
   const int64_t items = may_split ? p.row_tiles_upper * pieces : p.row_tiles_upper;
   if (items < p.items_upper) p.items_upper = (int32_t)items;
   if ((int64_t)p.items_upper * p.Hkv > kMaxRows) return LIME_UNSUPPORTED_SHAPE;      // (a round of CTAs past the last item stays inside 32 bits)
