@@ -267,8 +267,8 @@ LIME_API lime_status lime_norm_rotate(lime_ctx* ctx, const void* q, int64_t q_st
                              void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* cache_k, void* cache_v,
                              int64_t cache_rows, const int32_t* slots, int32_t* dev_flag, void* stream);
 
-/* Scratch for the two attention calls: enough for up to B users with `rows` query rows in all, whatever the lengths of their keys.
- * 0 on invalid arguments or before lime_set_sequence. */
+/* Scratch for the two attention calls: enough for every call of the shape set with at most B users and at most `rows` query rows in all,
+ * whatever the lengths of their keys.  0 on invalid arguments, before lime_set_sequence, and for more rows than a call takes. */
 LIME_API size_t lime_sequence_workspace_bytes(const lime_ctx* ctx, int32_t B, int64_t rows);
 
 /* Causal attention over packed histories:

@@ -1,4 +1,5 @@
 // C-ABI entry points of the sequence path: argument validation, workspace carving and launch sequencing.
+#include <algorithm>
 #include <cmath>
 
 #include "seq_common.cuh"
@@ -20,73 +21,70 @@ static lime_status ready(const Ctx* c) {
 }
 constexpr int64_t kMaxRows = 0x7fff0000LL;       // row indexes and the ends of the tiles that hold them stay inside 32 bits
 
-// Whether the rows go to k_seq_attn_few: up to 8 stacked rows a user on average that attend to nothing but the cache (`alone`).  On the
-// tensor cores' tiles of 128 rows instead: 64 events of 16 heads over 4 heads of 128 221 against 180 us, 256 of 4 over 4 of 32 53 against
-// 24.5, one of 8 over 2 of 64 17 against 11.6.
-static bool streams(const Ctx* c, int32_t B, int64_t rows, bool alone) {
+// How the rows of a batch are tiled, and by which kernel.
+//   STREAM: up to 8 stacked rows a user on average that attend to nothing but the cache (`alone`, bf16; k_seq_attn_few).  On the tensor
+//     cores' tiles of 128 rows instead: 64 events of 16 heads over 4 heads of 128 221 against 180 us, 256 of 4 over 4 of 32 53 against 24.5,
+//     one of 8 over 2 of 64 17 against 11.6.
+//   TENSOR: tensor cores (bf16), 128 stacked rows a CTA and two CTAs an SM, or two slots of 128 rows.
+//   CUDA16, CUDA64: CUDA cores (fp32), 16 stacked rows a tile where a user has no more on average, else 64 (64 for all, d_h = 64: 64 events of
+//     8 heads over 100..3000 rows 148, 16 100 us; three rows over 2000 36.9, 27.6).
+enum SeqForm { STREAM, TENSOR, CUDA16, CUDA64 };
+static SeqForm form_of(const Ctx* c, int32_t B, int64_t rows, bool alone) {
   const int G = c->seq.Hq / c->seq.Hkv;
-  return alone && c->cfg.dtype == LIME_BF16 && G <= 8 && rows * G <= 8ll * B;
+  if (c->cfg.dtype == LIME_BF16) return alone && G <= 8 && rows * G <= 8ll * B ? STREAM : TENSOR;
+  return G <= 16 && rows * G <= 16ll * B ? CUDA16 : CUDA64;
 }
-// How the rows of a batch are tiled, and how fine a batch may be cut (both attention calls).  Pieces are worth a merge where there are
-// few of them or little to merge; the figures are in us, the other choice first.
+// The tiles, and how fine a batch may be cut.  Pieces are worth a merge where there are few of them or little to merge; the figures are in
+// us, the other choice first.
 //   streamed rows: pieces of 4 tiles and more (2: 8 events over 500..5000 rows 25.6, now 18.0; 8: one event over 1000 14.0, 12.3), four a
 //     CTA (2: 64 events over 16..16384 235, 217; 8: 232);
 //   tensor cores: of 8 tiles and more, which cost a merge as much as 8 more (4 and 1: 64 events behind 16..8000 rows, 16 heads over 4 of 128
 //     119, 108; 2 and 1: 8 events of 16 heads over one of 64 41.2, 26.7; but a draft of 5 over 1000 rows 20.8, 21.9);
-//   CUDA cores, d_h = 64: 16 stacked rows a tile where a user has no more on average (64: 64 events of 8 heads over 100..3000 rows 148,
-//     100; three rows over 2000 36.9, 27.6); pieces of 2 tiles and more (4: 7 users' drafts 80.3, 73.8; the events 101, 90; the three rows
-//     27.4, 23.4).
-struct SeqTiling { int tok, kt, chunk_min, chunk_target, ctas; float item_cost, split_cost; bool few; };
-static SeqTiling tiling(const Ctx* c, int32_t B, int64_t rows, bool alone) {
+//   CUDA cores, d_h = 64: of 2 tiles and more (4: 7 users' drafts 80.3, 73.8; the events 101, 90; the three rows 27.4, 23.4).
+struct SeqTiling { int tok, kt, chunk_min, chunk_target, ctas; float item_cost, split_cost; };
+static SeqTiling tiling(const Ctx* c, SeqForm form) {
   const int G = c->seq.Hq / c->seq.Hkv;
+  const bool narrow = c->seq.d_h <= 64;
   SeqTiling t;
-  if (streams(c, B, rows, alone)) {
-    t.few = true;
+  if (form == STREAM) {
     t.tok = 8 / G;
     t.kt = 64;
     t.ctas = seq_few_blocks(c->seq.d_h) * kSMs;
     t.chunk_min = 4;
-    t.chunk_target = 4 * t.ctas;
     t.item_cost = 4.f;
     t.split_cost = 2.f;
-    return t;
-  }
-  if (c->cfg.dtype == LIME_BF16) {
-    // tensor cores: 128 stacked rows a CTA and two CTAs an SM, or two slots of 128 rows
-    const bool narrow = c->seq.d_h <= 64;
-    t.few = false;
+  } else if (form == TENSOR) {
     t.tok = (narrow ? 1 : 2) * (128 / G);
     t.kt = narrow ? 64 : 128;
     t.ctas = (narrow ? 2 : 1) * kSMs;
     t.chunk_min = 8;
-    t.chunk_target = 4 * t.ctas;
     t.item_cost = narrow ? 4.f : 6.f;
     t.split_cost = 8.f;
-    return t;
+  } else {
+    t.tok = (form == CUDA16 ? 16 : 64) / G;
+    t.kt = 64;
+    t.ctas = (narrow ? 2 : 1) * kSMs;
+    t.chunk_min = 2;
+    t.item_cost = 2.f;
+    t.split_cost = 1.f;
   }
-  // CUDA cores: 64 stacked rows a tile, or 16 where a user has no more on average
-  t.few = G <= 16 && rows * G <= 16ll * B;
-  t.tok = (t.few ? 16 : 64) / G;
-  t.kt = 64;
-  t.ctas = (c->seq.d_h <= 64 ? 2 : 1) * kSMs;
-  t.chunk_min = 2;
   t.chunk_target = 4 * t.ctas;
-  t.item_cost = 2.f;
-  t.split_cost = 1.f;
   return t;
 }
 
-// Carves the workspace; returns its size.  Row tiles: whole ones and one rest per user.  A row tile is cut into pieces of more than half
-// of what k_seq_schedule calls a chunk, and a chunk is at least 1 / chunk_target of all (row tile, key head) work, so pieces times key
-// heads are at most 2 * chunk_target, whatever the lengths.
-static size_t carve(SeqParams& p, const Ctx* c, int32_t B, int64_t rows, bool alone, void* base) {
-  const SeqTiling t = tiling(c, B, rows, alone);
+// Carves the workspace; returns its size, 0 where the lists would not count that many items.  Row tiles: whole ones and one rest per user.
+// A row tile is cut into pieces of more than half of what k_seq_schedule calls a chunk, and a chunk is at least 1 / chunk_target of all (row
+// tile, key head) work, so pieces times key heads are at most 2 * chunk_target, whatever the lengths.  For one form the size grows with B
+// and with rows.
+static size_t carve(SeqParams& p, const Ctx* c, SeqForm form, int32_t B, int64_t rows, void* base) {
+  const SeqTiling t = tiling(c, form);
   p.tok = t.tok; p.kt = t.kt; p.chunk_min = t.chunk_min; p.chunk_target = t.chunk_target;
   p.ctas = t.ctas; p.item_cost = t.item_cost; p.split_cost = t.split_cost;
-  const int64_t R = (int64_t)t.tok * p.G, pieces = 2ll * t.chunk_target / p.Hkv;
-  p.row_tiles_upper = (int32_t)(rows / t.tok + (B < rows ? B : rows));
-  p.items_upper = (int32_t)(p.row_tiles_upper + pieces);
-  p.split_upper = (int32_t)(pieces / 2 < p.row_tiles_upper ? pieces / 2 : p.row_tiles_upper);
+  const int64_t R = (int64_t)t.tok * p.G, pieces = 2ll * t.chunk_target / p.Hkv, row_tiles = rows / t.tok + (B < rows ? B : rows);
+  if (row_tiles + pieces > kMaxRows) return 0;
+  p.row_tiles_upper = (int32_t)row_tiles;
+  p.items_upper = (int32_t)(row_tiles + pieces);
+  p.split_upper = (int32_t)(pieces / 2 < row_tiles ? pieces / 2 : row_tiles);
   size_t o = 0;
   char* at = static_cast<char*>(base);
   auto take = [&](size_t n) { void* r = at ? at + o : nullptr; o += (n + 255) & ~(size_t)255; return r; };
@@ -110,9 +108,10 @@ static SeqParams shape(const Ctx* c) {
 }
 
 static lime_status attend(const Ctx* c, SeqParams& p, bool tree, void* ws, size_t ws_bytes, cudaStream_t st) {
-  const bool alone = tree && p.k == nullptr;
+  const SeqForm form = form_of(c, p.B, p.q_rows, tree && p.k == nullptr);
   char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
-  const size_t need = carve(p, c, p.B, p.q_rows, alone, base);
+  const size_t need = carve(p, c, form, p.B, p.q_rows, base);
+  if (need == 0) return LIME_UNSUPPORTED_SHAPE;
   if (ws == nullptr || ws_bytes < need + (size_t)(base - static_cast<char*>(ws))) return LIME_WORKSPACE_TOO_SMALL;
   // what the host knows of the keys bounds the pieces as well
   const int64_t most = tree ? (int64_t)p.max_pages * p.page_rows + (p.k ? p.q_rows + p.kt : 0) : p.kv_rows;
@@ -125,8 +124,8 @@ static lime_status attend(const Ctx* c, SeqParams& p, bool tree, void* ws, size_
   if ((int64_t)p.items_upper * p.Hkv > kMaxRows) return LIME_UNSUPPORTED_SHAPE;      // (a round of CTAs past the last item stays inside 32 bits)
   lime_status s;
   if ((s = launch_seq_schedule(p, tree, st)) != LIME_OK) return s;
-  if (c->cfg.dtype != LIME_BF16) s = launch_seq_attn_simt(p, tree, tiling(c, p.B, p.q_rows, alone).few, st);
-  else if (streams(c, p.B, p.q_rows, alone)) s = launch_seq_attn_few(p, st);
+  if (c->cfg.dtype != LIME_BF16) s = launch_seq_attn_simt(p, tree, form == CUDA16, st);
+  else if (form == STREAM) s = launch_seq_attn_few(p, st);
   else s = p.dh <= 64 ? launch_seq_attn_d64_tc(p, tree, st) : launch_seq_attn_tc(p, tree, st);
   if (s != LIME_OK) return s;
   return may_split ? launch_seq_merge(p, c->cfg.dtype, st) : LIME_OK;
@@ -188,9 +187,23 @@ size_t lime_sequence_workspace_bytes(const lime_ctx* ctx, int32_t B, int64_t row
   if (!ctx || B < 0 || rows < 0 || rows > kMaxRows) return 0;
   const Ctx* c = reinterpret_cast<const Ctx*>(ctx);
   if (!c->have_seq) return 0;
-  SeqParams p = shape(c);
-  const size_t any = carve(p, c, B, rows, false, nullptr), alone = carve(p, c, B, rows, true, nullptr);
-  return (any > alone ? any : alone) + 256;
+  // Every form that a call of at most B users and rows can take, with the most users and rows that it can have then.  Fewer users may need
+  // more: their rows are then many enough for larger tiles.
+  const int64_t G = c->seq.Hq / c->seq.Hkv;
+  const struct { SeqForm form; bool can; int64_t B, rows; } forms[4] = {
+      {STREAM, c->cfg.dtype == LIME_BF16 && G <= 8, B, std::min(rows, 8 * (int64_t)B / G)},
+      {TENSOR, c->cfg.dtype == LIME_BF16, B, rows},
+      {CUDA16, c->cfg.dtype != LIME_BF16 && G <= 16, B, std::min(rows, 16 * (int64_t)B / G)},
+      {CUDA64, c->cfg.dtype != LIME_BF16, G <= 16 && rows > 0 ? std::min((int64_t)B, (rows * G - 1) / 16) : B, rows}};
+  size_t most = 0;
+  for (const auto& f : forms) {
+    if (!f.can || (f.form == CUDA64 && G <= 16 && rows * G <= 16)) continue;
+    SeqParams p = shape(c);
+    const size_t n = carve(p, c, f.form, (int32_t)f.B, f.rows, nullptr);
+    if (n == 0) return 0;
+    most = std::max(most, n);
+  }
+  return most + 256;
 }
 
 lime_status lime_attend_history(lime_ctx* ctx, const void* q, int64_t q_stride, const int32_t* off, const void* k, int64_t k_stride,
