@@ -276,8 +276,9 @@ LIME_API size_t lime_sequence_workspace_bytes(const lime_ctx* ctx, int32_t B, in
  * of i's user (i, j counted within the user): the last query sees every key, so new rows behind older ones are queries fewer than
  * keys.  q [q_rows x Hq x d_h] by off, k and v [kv_rows x Hkv x d_h] by kv_off (NULL: the same rows as the queries', kv_rows =
  * q_rows); out [q_rows x Hq x d_h], which overlaps no input.  A query that sees no key (more queries than keys, an empty history) gets zeros.  What a query does
- * not see has no influence on it, infinities and NaN included.  bf16: products of bf16 values in fp32, probabilities rounded to bf16 for
- * the value product (their sum is not), one rounding of the result; fp32: all in fp32. */
+ * not see has no influence on it, infinities and NaN included; what it sees has the influence that the formula gives: NaN where a score is
+ * NaN or +infinity, or where all are -infinity.  bf16: products of bf16 values in fp32, probabilities rounded to bf16 for the value product
+ * (their sum is not), one rounding of the result; fp32: all in fp32. */
 LIME_API lime_status lime_attend_history(lime_ctx* ctx, const void* q, int64_t q_stride, const int32_t* off, const void* k,
                                 int64_t k_stride, const void* v, int64_t v_stride, const int32_t* kv_off, int32_t B, int64_t q_rows,
                                 int64_t kv_rows, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);

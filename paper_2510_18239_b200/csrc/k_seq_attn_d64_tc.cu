@@ -340,7 +340,7 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             p.part_ml[piece * 2 * R + r] = m == -INFINITY ? m : m * scale;
             p.part_ml[(piece * 2 + 1) * R + r] = l;
           }
-          const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+          const float inv = !whole ? 1.f : seq_inverse(l, TREE ? it.b > 0 || p.k != nullptr : it.c + tok > 0);
           const int64_t to = !valid ? -1 : whole ? (int64_t)(it.row0 + tok) * p.out_stride + (kvh * G + r % G) * p.dh : (piece * R + r) * p.dh;
           float z = 0.f;
 #pragma unroll 1

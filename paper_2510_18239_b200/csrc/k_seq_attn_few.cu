@@ -171,6 +171,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, seq_few_blocks(DHP)) k_seq_att
     }
     // the next item is looked up while this one is joined
     const int row0 = it.row0, part = it.part, was_rows = rows, was_kvh = kvh;
+    const bool any = it.t0 < it.t1;
     work = next_work();
     if (work >= 0) it = seq_item(p, work);
     l += __shfl_xor_sync(0xffffffffu, l, 1);
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, seq_few_blocks(DHP)) k_seq_att
       }
       if (at >= p.dh) continue;
       if (part < 0) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const float inv = seq_inverse(sum, any);
         __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.out) + (int64_t)(row0 + r / G) * p.out_stride + (was_kvh * G + r % G) * p.dh + at;
         *reinterpret_cast<uint2*>(to) = make_uint2(seq_pack(acc.x * inv, acc.y * inv), seq_pack(acc.z * inv, acc.w * inv));
       } else {

@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(256, DHP <= 64 ? 2 : 1) k_seq_attn_simt(const 
     const int r = ty + 16 * i;
     if (r >= rows) continue;
     if (it.part < 0) {
-      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+      const float inv = seq_inverse(l[i], TREE ? it.b > 0 || p.k != nullptr : it.c + r / G > 0);
       float* o = static_cast<float*>(p.out) + (int64_t)(it.row0 + r / G) * p.out_stride + (kvh * G + r % G) * p.dh;
 #pragma unroll
       for (int c = 0; c < DC; ++c)

@@ -469,7 +469,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             p.part_ml[part * 2 * R + pr] = m == -INFINITY ? m : m * scale;
             p.part_ml[(part * 2 + 1) * R + pr] = l;
           }
-          const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+          const float inv = !whole ? 1.f : seq_inverse(l, TREE ? w.it.b > 0 || p.k != nullptr : w.it.c + tok > 0);
           w0 *= inv; w1 *= inv;
           // where this row goes (element offset in the output, or in the partial results); -1: nowhere
           const int64_t to = !valid ? -1 : whole ? (int64_t)(w.it.row0 + tok) * p.out_stride + (kvh * G + r % G) * p.dh : (part * R + pr) * p.dh;

@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(256, 2) k_seq_merge(const SeqParams p) {
           acc.x = fmaf(w, a[u].x, acc.x); acc.y = fmaf(w, a[u].y, acc.y); acc.z = fmaf(w, a[u].z, acc.z); acc.w = fmaf(w, a[u].w, acc.w);
         }
       }
-      const float inv = total == 0.f ? 0.f : 1.f / total;
+      const float inv = seq_inverse(total, true);                 // (a row tile that is cut has more key tiles than its rows could miss)
       T* o = static_cast<T*>(p.out) + (int64_t)(sp.row0 + r / p.G) * p.out_stride + (kvh * p.G + r % p.G) * p.dh + lane * 4;
       if (mine) { Store<T>::st(o, acc.x * inv); Store<T>::st(o + 1, acc.y * inv); Store<T>::st(o + 2, acc.z * inv); Store<T>::st(o + 3, acc.w * inv); }
     }

@@ -5,8 +5,9 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import sequence_oracle as so
 from paper_2510_18239_b200 import binding
-from test_gpu_sequence import check_history, check_tree, lime, off_of, paged, rand
+from test_gpu_sequence import check_history, check_tree, close, f64, lime, off_of, paged, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +79,60 @@ def test_scratch_of_absurd_batches():
     m = lime("bf16", 8, 1, 8)
     assert binding.lime_sequence_workspace_bytes(m.ctx, 2 ** 31 - 1, 0x7fff0000) == 0
     assert binding.lime_sequence_workspace_bytes(m.ctx, 2 ** 31 - 1, 1) > 0
+
+
+def infinite_scores(q, at, k, bad):
+    """Feature 0 decides the sign of a score against the key rows `at`, whose feature 0 is `bad`: the one for even query heads, the other for odd."""
+    q[:, 0::2, 0], q[:, 1::2, 0] = 1.0, -1.0
+    k[at, :, 0] = bad
+
+
+def check_infinite(got, q, k, v, sees, at, bad, scale, dh, dtype):
+    """A row and head that sees a key with score +inf, or none with a finite one, has NaN (inf - inf); a score of -inf is a probability of 0."""
+    Hq = q.shape[1]
+    hot = np.zeros(k.shape[0], bool)
+    hot[at] = True
+    cold = k.copy()
+    cold[hot] = 0.0
+    ref, mag, size = so.attend(q, cold, v, sees & ~hot, scale)
+    for h in range(Hq):
+        positive = (bad > 0) == (h % 2 == 0)
+        nan = (sees & hot).any(1) if positive else sees.any(1) & ~(sees & ~hot).any(1)
+        assert torch.isnan(got[:, h][torch.from_numpy(nan).to(got.device)]).all()
+        rest = np.flatnonzero(~nan)
+        close(got[rest.tolist(), h:h + 1], ref[rest, h:h + 1], mag[rest, h:h + 1], size[rest, h:h + 1], dh, k.shape[0], dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf")])
+@pytest.mark.parametrize("Hq,Hkv,dh", [(2, 1, 64), (4, 4, 32), (2, 2, 128)])
+def test_infinite_scores(dtype, bad, Hq, Hkv, dh):
+    gen = torch.Generator().manual_seed(67)
+    m, scale = lime(dtype, Hq, Hkv, dh), 1 / np.sqrt(dh)
+    # causal: user 0 begins with such a key and has another further on, user 1 has one in the middle; user 2 has more queries than keys
+    nq, nk, at = [150, 140, 9], [150, 140, 4], [[0, 90], [70], [0]]
+    q, k, v = rand(gen, sum(nq), Hq, dh, dtype=dtype), rand(gen, sum(nk), Hkv, dh, dtype=dtype), rand(gen, sum(nk), Hkv, dh, dtype=dtype)
+    infinite_scores(q, [j + a for j, i in zip((0, 150, 290), at) for a in i], k, bad)
+    got = m.attend_history(q.cuda(), k.cuda(), v.cuda(), off_of(nq), kv_off=off_of(nk))
+    i = j = 0
+    for a, b, hot in zip(nq, nk, at):
+        check_infinite(got[i:i + a], f64(q[i:i + a]), f64(k[j:j + b]), f64(v[j:j + b]), so.causal(a, b), hot, bad, scale, dh, dtype)
+        i, j = i + a, j + b
+    # over the cache: nothing but such keys, in one tile and in pieces that are joined; one among many; one alone; no keys
+    c = [1, 100, 5000, 3000, 0, 5000]
+    hot = [range(1), range(100), range(5000), [2999], [], [0, 777, 4999]]
+    for n, form in (([1] * 6, "none"), ([3] * 6, "roots"), ([20] * 6, "none")):
+        ck, cv, table = paged(gen, c, 64, Hkv, dh, dtype)
+        q, tk, tv = (rand(gen, sum(n), h, dh, dtype=dtype) for h in (Hq, Hkv, Hkv))
+        flat = ck.view(-1, Hkv, dh)
+        infinite_scores(q, [int(table[b, j // 64]) * 64 + j % 64 for b in range(6) for j in hot[b]], flat, bad)
+        new = {} if form == "none" else dict(tree_k=tk.cuda(), tree_v=tv.cuda())
+        got = m.attend_tree(q.cuda(), ck.cuda(), cv.cuda(), table.cuda(), torch.tensor(c, dtype=torch.int32).cuda(), off_of(n), **new)
+        i = 0
+        for b, (a, cb) in enumerate(zip(n, c)):
+            kk, vv = so.cached_rows(f64(ck), table[b].tolist(), cb), so.cached_rows(f64(cv), table[b].tolist(), cb)
+            sees = np.ones((a, cb), bool)
+            if form == "roots":
+                kk, vv, sees = np.concatenate((kk, f64(tk[i:i + a]))), np.concatenate((vv, f64(tv[i:i + a]))), np.concatenate((sees, np.eye(a, dtype=bool)), 1)
+            check_infinite(got[i:i + a], f64(q[i:i + a]), kk, vv, sees, list(hot[b]), bad, scale, dh, dtype)
+            i += a
