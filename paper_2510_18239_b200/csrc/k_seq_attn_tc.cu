@@ -296,7 +296,10 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             const SeqTile k = seq_tile<TREE>(p, w.it, w.n_tree, t);
             if (!w.mended(k, again)) continue;
             const int st = (g + 1) % STAGES;
-            if (!__all_sync(0xffffffffu, mbar_wait(mend_ask, mend_ph, p.err, 119) &&
+            // The tiles and items before the next one to be mended may take seconds (histories that fill their tiles, then one that does not).
+            // They are not this warp's to watch: what gets stuck is seen by a warp that waits for a step of it, and the error word ends this
+            // wait too.
+            if (!__all_sync(0xffffffffu, mbar_wait_limit(mend_ask, mend_ph, p.err, 119, 60 * kWaitLimitNs) &&
                                              mbar_wait(&kv_full[st], (uint32_t)((g + 1) / STAGES) & 1u, p.err, 118))) { ok = false; break; }
             mend_ph ^= 1u;
             uint8_t* tile = smem + C::OFF_KV + st * C::TILE;

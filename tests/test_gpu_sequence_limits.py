@@ -136,3 +136,36 @@ def test_infinite_scores(dtype, bad, Hq, Hkv, dh):
                 kk, vv, sees = np.concatenate((kk, f64(tk[i:i + a]))), np.concatenate((vv, f64(tv[i:i + a]))), np.concatenate((sees, np.eye(a, dtype=bool)), 1)
             check_infinite(got[i:i + a], f64(q[i:i + a]), kk, vv, sees, list(hot[b]), bad, scale, dh, dtype)
             i += a
+
+
+def test_a_call_of_seconds_whose_first_ragged_tile_comes_last():
+    """The first user's history fills its key tiles, which leaves nothing to mend in them for longer than a wait may take; the second's,
+    whose few rows come last, ends inside one."""
+    Hq, dh, page, n, c = 16, 128, 128, [180000, 4000], [1 << 21, 100]
+    m = lime("bf16", Hq, 1, dh)
+    gen = torch.Generator(device="cuda").manual_seed(71)
+    normal = lambda *s: torch.randn(s, generator=gen, device="cuda").to(torch.bfloat16)
+    pages = c[0] // page + 1
+    ck, cv, q = normal(pages, page, 1, dh), normal(pages, page, 1, dh), normal(sum(n), Hq, dh)
+    cv[-1, c[1]:] = float("nan")
+    table = torch.full((2, pages - 1), -1, dtype=torch.int32)
+    table[0], table[1, 0] = torch.arange(pages - 1), pages - 1
+    out = torch.empty_like(q)
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    args = (ck, cv, table.cuda(), torch.tensor(c, dtype=torch.int32).cuda(), off_of(n))
+    begin.record()
+    m.attend_tree(q, *args, out=out)
+    end.record()
+    torch.cuda.synchronize()
+    assert binding.lime_device_status(m.ctx) == 0
+    assert begin.elapsed_time(end) > 2200                        # or the case no longer outlasts a wait
+    assert torch.isfinite(out).all()
+    # rows of both ends: |out - ref| is bounded as in test_gpu_sequence.py; A = sum p |v| from the same sum
+    for b, first in ((0, 0), (1, n[0])):
+        rows = [first, first + n[b] // 2, first + n[b] - 1]
+        kk, vv = (x.view(-1, dh)[:c[0]] if b == 0 else x[-1, :c[1], 0] for x in (ck, cv))
+        for r in rows:
+            s = q[r].double() @ kk.double().T / np.sqrt(dh)
+            p = torch.softmax(s, -1)
+            size = (q[r].double().abs() @ kk.double().abs().T).amax(-1) / np.sqrt(dh)
+            close(out[r:r + 1], (p @ vv.double()).cpu().numpy()[None], (p @ vv.double().abs()).cpu().numpy()[None], size.cpu().numpy()[None], dh, c[b], "bf16")
