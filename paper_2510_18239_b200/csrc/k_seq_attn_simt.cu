@@ -228,12 +228,14 @@ __global__ void __launch_bounds__(256, DHP <= 64 ? 2 : 1) k_seq_attn_simt(const 
     __syncwarp();
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
+  // the first row that sees a key
+  const int seeing = TREE ? (it.b > 0 || p.k != nullptr ? 0 : RT) : min(max(1 - it.c, 0), RT) * G;
 #pragma unroll
   for (int i = 0; i < RI; ++i) {
     const int r = ty + 16 * i;
     if (r >= rows) continue;
     if (it.part < 0) {
-      const float inv = seq_inverse(l[i], TREE ? it.b > 0 || p.k != nullptr : it.c + r / G > 0);
+      const float inv = seq_inverse(l[i], r >= seeing);
       float* o = static_cast<float*>(p.out) + (int64_t)(it.row0 + r / G) * p.out_stride + (kvh * G + r % G) * p.dh;
 #pragma unroll
       for (int c = 0; c < DC; ++c)

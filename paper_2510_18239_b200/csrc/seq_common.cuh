@@ -88,9 +88,9 @@ __device__ __forceinline__ int64_t seq_page(const SeqParams& p, int user, int j)
   return p.n_pages;
 }
 
-// What a result is multiplied by: a sum of probabilities is 0 only where no score is finite or above; such a row sees nothing and gets zeros,
-// or it sees scores of -infinity alone, whose softmax is NaN.
-__device__ __forceinline__ float seq_inverse(float sum, bool sees) { return sum != 0.f ? 1.f / sum : sees ? __int_as_float(0x7fffffff) : 0.f; }
+// What a result is multiplied by: 0 where the row sees nothing.  A row that sees scores of -infinity alone has a sum of 0 and values of 0,
+// which the reciprocal makes NaN, as the formula has it.
+__device__ __forceinline__ float seq_inverse(float sum, bool sees) { return sees ? 1.f / sum : 0.f; }
 
 // blocks of k_seq_attn_few an SM (as many as fit without spilling much; 8 rather than 6 at d_h <= 32: 24.5 against 30.7 us for 256 events over
 // 512 rows, 3 rather than 2 at d_h > 64: 180 against 201 us for 64 events over 16..16384)
