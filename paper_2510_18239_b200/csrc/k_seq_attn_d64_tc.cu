@@ -334,7 +334,7 @@ k_seq_attn_d64_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         tc_fence_after();
         if (any_valid) {
           const bool whole = it.part < 0;
-          const int R = p.tok * G, kvh = at.work % p.Hkv, tok = min(r, it.rows * G - 1) / G;
+          const int R = p.part_rows, kvh = at.work % p.Hkv, tok = min(r, it.rows * G - 1) / G;
           const int64_t piece = (int64_t)it.part * p.Hkv + kvh;
           if (!whole && valid) {
             p.part_ml[piece * 2 * R + r] = m == -INFINITY ? m : m * scale;

@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, seq_few_blocks(DHP)) k_seq_att
   pdl_wait();
   pdl_launch_dependents();
   const __nv_bfloat16 *q = static_cast<const __nv_bfloat16*>(p.q), *ck = static_cast<const __nv_bfloat16*>(p.ck), *cv = static_cast<const __nv_bfloat16*>(p.cv);
-  const int n_work = p.plan->n_items * p.Hkv, G = p.G, R = p.tok * G;
+  const int n_work = p.plan->n_items * p.Hkv, G = p.G, R = p.part_rows;
   const int64_t step = (int64_t)p.Hkv * p.dh;
   int turn = 0;
   auto next_work = [&]() {                         // back and forth; -1: the end

@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(256, DHP <= 64 ? 2 : 1) k_seq_attn_simt(const 
 #pragma unroll
           for (int e = 0; e < VW; ++e) o[c * 16 * VW + tx * VW + e] = acc[i][c * VW + e] * inv;
     } else {
-      const int R = p.tok * G;
+      const int R = p.part_rows;
       const int64_t at = (int64_t)it.part * p.Hkv + kvh;
       if (tx == 0) { p.part_ml[at * 2 * R + r] = m[i]; p.part_ml[(at * 2 + 1) * R + r] = l[i]; }
       float* o = p.part_acc + (at * R + r) * p.dh;

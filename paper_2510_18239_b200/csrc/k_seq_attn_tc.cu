@@ -467,7 +467,7 @@ k_seq_attn_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           const int c_lo = w.same ? s * (DHP / 2) : 0, c_hi = min(w.same ? c_lo + DHP / 2 : DHP, p.dh);
           const bool whole = w.it.part < 0;
           const int64_t part = (int64_t)w.it.part * p.Hkv + kvh;
-          const int R = p.tok * G, pr = w.first_token(s) * G + r;
+          const int R = p.part_rows, pr = w.first_token(s) * G + r;
           if (!whole && valid && (s == 0 || !w.same)) {
             p.part_ml[part * 2 * R + pr] = m == -INFINITY ? m : m * scale;
             p.part_ml[(part * 2 + 1) * R + pr] = l;

@@ -189,7 +189,7 @@ lime_status launch_seq_schedule(const SeqParams& p, bool tree, cudaStream_t st) 
 template <typename T>
 __global__ void __launch_bounds__(256, 2) k_seq_merge(const SeqParams p) {
   pdl_wait();
-  const int lane = threadIdx.x & 31, R = p.tok * p.G, pairs = p.plan->n_split * p.Hkv;
+  const int lane = threadIdx.x & 31, R = p.part_rows, pairs = p.plan->n_split * p.Hkv;
   const bool mine = lane * 4 < p.dh;
   for (int i = blockIdx.x; i < pairs; i += gridDim.x) {
     const int kvh = i % p.Hkv;
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(256, 2) k_seq_merge(const SeqParams p) {
 
 lime_status launch_seq_merge(const SeqParams& p, int dtype, cudaStream_t st) {
   const int64_t pairs = (int64_t)p.split_upper * p.Hkv;
-  const dim3 grid((unsigned)(pairs < 2 * kSMs ? pairs : 2 * kSMs), (unsigned)((p.tok * p.G + 31) / 32));
+  const dim3 grid((unsigned)(pairs < 2 * kSMs ? pairs : 2 * kSMs), (unsigned)((p.part_rows + 31) / 32));
   ProfScope _p("k_seq_merge", st);
   if (dtype == LIME_BF16) launch_pdl(k_seq_merge<__nv_bfloat16>, grid, dim3(256), 0, st, p);
   else launch_pdl(k_seq_merge<float>, grid, dim3(256), 0, st, p);

@@ -73,18 +73,21 @@ static SeqTiling tiling(const Ctx* c, SeqForm form) {
 }
 
 // Carves the workspace; returns its size, 0 where the lists would not count that many items.  Row tiles: whole ones and one rest per user.
-// A row tile is cut into pieces of more than half of what k_seq_schedule calls a chunk, and a chunk is at least 1 / chunk_target of all (row
-// tile, key head) work, so pieces times key heads are at most 2 * chunk_target, whatever the lengths.  For one form the size grows with B
-// and with rows.
+// What k_seq_schedule calls a chunk is at least 1 / chunk_target of all (row tile, key head) work, so the row tiles longer than that, which
+// it cuts, are fewer than chunk_target / Hkv, and a row tile has at most one piece more than chunks: pieces are bounded whatever the
+// lengths, and each holds no more rows than the call has (one event of 16 over 4 heads of 128 3.8 MB; 158 with whole tiles and twice the
+// chunks).  For one form the size grows with B and with rows.
 static size_t carve(SeqParams& p, const Ctx* c, SeqForm form, int32_t B, int64_t rows, void* base) {
   const SeqTiling t = tiling(c, form);
   p.tok = t.tok; p.kt = t.kt; p.chunk_min = t.chunk_min; p.chunk_target = t.chunk_target;
   p.ctas = t.ctas; p.item_cost = t.item_cost; p.split_cost = t.split_cost;
-  const int64_t R = (int64_t)t.tok * p.G, pieces = 2ll * t.chunk_target / p.Hkv, row_tiles = rows / t.tok + (B < rows ? B : rows);
+  const int64_t row_tiles = rows / t.tok + (B < rows ? B : rows), cut = std::min(row_tiles, (int64_t)t.chunk_target / p.Hkv);
+  const int64_t pieces = t.chunk_target / p.Hkv + cut;
   if (row_tiles + pieces > kMaxRows) return 0;
   p.row_tiles_upper = (int32_t)row_tiles;
   p.items_upper = (int32_t)(row_tiles + pieces);
-  p.split_upper = (int32_t)(pieces / 2 < row_tiles ? pieces / 2 : row_tiles);
+  p.split_upper = (int32_t)cut;
+  p.part_rows = (int32_t)std::min((int64_t)t.tok, rows) * p.G;
   size_t o = 0;
   char* at = static_cast<char*>(base);
   auto take = [&](size_t n) { void* r = at ? at + o : nullptr; o += (n + 255) & ~(size_t)255; return r; };
@@ -92,9 +95,9 @@ static size_t carve(SeqParams& p, const Ctx* c, SeqForm form, int32_t B, int64_t
   p.tile_start = (int32_t*)take(((size_t)B + 1) * 4);
   p.items = (SeqItem*)take((size_t)p.items_upper * sizeof(SeqItem));
   p.splits = (SeqSplit*)take((size_t)p.split_upper * sizeof(SeqSplit));
-  const size_t parts = (size_t)pieces * p.Hkv * R;
-  p.part_ml = (float*)take(parts * 2 * 4);
-  p.part_acc = (float*)take(parts * p.dh * 4);
+  const size_t part_rows = cut > 0 ? (size_t)pieces * p.Hkv * p.part_rows : 0;
+  p.part_ml = (float*)take(part_rows * 2 * 4);
+  p.part_acc = (float*)take(part_rows * p.dh * 4);
   return o;
 }
 
@@ -116,8 +119,7 @@ static lime_status attend(const Ctx* c, SeqParams& p, bool tree, void* ws, size_
   // what the host knows of the keys bounds the pieces as well
   const int64_t most = tree ? (int64_t)p.max_pages * p.page_rows + (p.k ? p.q_rows + p.kt : 0) : p.kv_rows;
   const int64_t tiles = (most + p.kt - 1) / p.kt + 1, pieces = (tiles - 1) / p.chunk_min + 1;
-  // (with more heads of keys than chunk_target no row tile can be: a chunk is then longer than all of them together, and there is no room
-  // in the list of them)
+  // (with more heads of keys than chunk_target no row tile can be: a chunk is then longer than all of them together)
   const bool may_split = tiles > p.chunk_min && p.split_upper > 0;
   const int64_t items = may_split ? p.row_tiles_upper * pieces : p.row_tiles_upper;
   if (items < p.items_upper) p.items_upper = (int32_t)items;

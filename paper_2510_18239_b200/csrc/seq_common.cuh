@@ -40,8 +40,9 @@ struct SeqParams {
   int32_t tok, kt;                       // tokens per row tile, keys per key tile
   // workspace
   SeqPlan* plan; SeqItem* items; SeqSplit* splits; int32_t* tile_start;
-  float *part_ml, *part_acc;             // [part][kvh][2][tok * G] and [part][kvh][tok * G][dh]
+  float *part_ml, *part_acc;             // [part][kvh][2][part_rows] and [part][kvh][part_rows][dh]
   int32_t row_tiles_upper, items_upper, split_upper;
+  int32_t part_rows;                     // stacked rows a row tile of the call can have
   // how row tiles are cut: key tiles per item at least; items (over all key heads) that a batch may make about; CTAs that run at once; what
   // an item costs besides its key tiles, and what its being one of several adds, in key tiles
   int32_t chunk_min, chunk_target, ctas;

@@ -81,6 +81,14 @@ def test_scratch_of_absurd_batches():
     assert binding.lime_sequence_workspace_bytes(m.ctx, 2 ** 31 - 1, 1) > 0
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hq,Hkv,dh", [(8, 2, 64), (4, 4, 32), (16, 4, 128)])
+def test_scratch_goes_by_the_rows(dtype, Hq, Hkv, dh):
+    """Partial results are kept for the rows that there are, not for whole tiles: one event takes a few MB, as every call has its own."""
+    m = lime(dtype, Hq, Hkv, dh)
+    assert binding.lime_sequence_workspace_bytes(m.ctx, 1, 1) < 4 << 20
+
+
 def infinite_scores(q, at, k, bad):
     """Feature 0 decides the sign of a score against the key rows `at`, whose feature 0 is `bad`: the one for even query heads, the other for odd."""
     q[:, 0::2, 0], q[:, 1::2, 0] = 1.0, -1.0
