@@ -98,18 +98,26 @@ __device__ __noinline__ void seq_add_not_finite(const SeqParams& p, int work, in
   const int kvh = work % p.Hkv, n_tree = TREE ? seq_tree_tiles(p, it) : 0;
   const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v);
   auto add = [&](const __nv_bfloat16* row) {
-    for (int c = 0; c < 32; ++c)
-      if (c0 + c < p.dh) {
-        const float x = __bfloat162float(row[c0 + c]);
-        if (!(fabsf(x) < INFINITY)) a[c] += x;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (c0 + u * 8 >= p.dh) break;
+      const uint4 x = *reinterpret_cast<const uint4*>(row + c0 + u * 8);
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xffff0000u);
+        if (!(fabsf(lo) < INFINITY)) a[u * 8 + 2 * e] += lo;
+        if (!(fabsf(hi) < INFINITY)) a[u * 8 + 2 * e + 1] += hi;
       }
+    }
   };
+  int anc = it.c + token;                                  // the chain of ancestors is walked once, as its tiles come from the last one back
   for (int t = lo; t < hi; ++t) {
     const SeqTile k = seq_tile<TREE>(p, it, n_tree, t);
     if (!seq_masked(it, k, p.kt)) continue;
     if (TREE && k.kind == 2) {
-      for (int j = it.c + token; j >= k.j0; j = seq_parent(p, it.row0 - it.c, j))
-        if (j < k.j0 + p.kt) add(v + (int64_t)(it.row0 - it.c + j) * p.v_stride + kvh * p.dh);
+      for (; anc >= k.j0; anc = seq_parent(p, it.row0 - it.c, anc))
+        if (anc < k.j0 + p.kt) add(v + (int64_t)(it.row0 - it.c + anc) * p.v_stride + kvh * p.dh);
     } else {
       const int end = min(k.j0 + p.kt, TREE ? k.n : it.c + token);
       for (int j = k.j0; j < end; ++j) {

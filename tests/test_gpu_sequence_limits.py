@@ -146,6 +146,26 @@ def test_infinite_scores(dtype, bad, Hq, Hkv, dh):
             i += a
 
 
+@pytest.mark.parametrize("Hq,Hkv,dh", [(2, 1, 32), (2, 1, 64), (1, 1, 128)])
+def test_values_that_are_not_finite_in_a_long_chain(Hq, Hkv, dh):
+    """Causal rows as a chain of drafts, with a NaN and an infinity among the first values: what every later row adds of them takes a walk up
+    its chain, not one for every tile of it, which would keep the warps that wait for its result longer than they may."""
+    n, m = 100000, lime("bf16", Hq, Hkv, dh)
+    gen = torch.Generator(device="cuda").manual_seed(73)
+    q, k, v = (torch.randn(n, h, dh, generator=gen, device="cuda").to(torch.bfloat16) for h in (Hq, Hkv, Hkv))
+    page = torch.zeros(1, 16, Hkv, dh, dtype=torch.bfloat16, device="cuda")
+    args = (page, page, torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), off_of([n]))
+    chain = torch.arange(-1, n - 1, dtype=torch.int32, device="cuda")
+    clean = m.attend_tree(q, *args, parent=chain, tree_k=k, tree_v=v)
+    v[300, :, 1], v[70, :, 5] = float("nan"), float("inf")
+    got = m.attend_tree(q, *args, parent=chain, tree_k=k, tree_v=v)
+    assert binding.lime_device_status(m.ctx) == 0
+    assert torch.isnan(got[300:, :, 1]).all() and torch.equal(got[:300, :, 1], clean[:300, :, 1])
+    assert (got[70:, :, 5] == float("inf")).all() and torch.equal(got[:70, :, 5], clean[:70, :, 5])
+    rest = [c for c in range(dh) if c not in (1, 5)]
+    assert torch.equal(got[:, :, rest], clean[:, :, rest])
+
+
 def test_a_call_of_seconds_whose_first_ragged_tile_comes_last():
     """The first user's history fills its key tiles, which leaves nothing to mend in them for longer than a wait may take; the second's,
     whose few rows come last, ends inside one."""
