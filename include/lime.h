@@ -226,10 +226,10 @@ LIME_API lime_status lime_score_candidates_head(lime_ctx* ctx, const void* link_
                                        void* ws, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------------------------------------
- * The user encoder that LIME is measured against (the paper's softmax "skyline"): every event of a history attends to the events
- * before it, candidates or drafted continuations attend to the history and to themselves, and the history's keys and values stay in
- * a cache between requests.  Three calls, for inference: norms and rotation on the way into the cache, attention over whole histories,
- * attention of a few new rows over the cache.
+ * Attention over the whole history, which LIME replaces (the paper's softmax "skyline" attends so): every event of a history attends to
+ * the events before it, candidates attend to the history and to themselves.  Three calls, for inference: norms and rotation on the way
+ * into a cache, attention over whole histories, attention of a few new rows over the cache.  The norms of heads, the rotation by
+ * position, the cache in pages and the trees of drafted rows are this library's own, the paper has none of them.
  *
  * Rows are packed user after user: row t of a tensor of h heads is h * d_h contiguous elements of config.dtype (head after head) at
  * t * stride; strides are in elements, at least h * d_h and a multiple of 16 bytes, so queries, keys and values may be parts of one
@@ -251,8 +251,9 @@ LIME_API lime_status lime_set_sequence(lime_ctx* ctx, const lime_sequence* seq);
 
 /* Norm of each head and rotation by position, in one pass:
  *   y = x * rsqrt(mean(x^2) + norm_eps) * gamma,  then each pair (a, b) of y to (a cos - b sin, b cos + a sin)
- * for q [rows x Hq x d_h] and k [rows x Hkv x d_h]; statistics, angles and products in 32 bits or more, one rounding at the end.  The
- * angle is formed from the whole position in fixed point, so positions far out lose nothing; negative ones turn backwards.
+ * for q [rows x Hq x d_h] and k [rows x Hkv x d_h]; statistics, angles and products in 32 bits or more, one rounding at the end.  (The
+ * sum of squares is fp32: a head with features of 1e18 and more in magnitude may come out as zeros.)  The angle is formed from the whole
+ * position in fixed point, so positions far out lose nothing; negative ones turn backwards.
  * gamma_q / gamma_k [d_h] in config.dtype, NULL = ones.  positions [rows] device int32 (may be NULL with rot_dim = 0).
  * q_out, k_out [rows x ..] with strides of their own; each may be its input itself (same pointer and stride), and overlaps nothing else
  * that is read or written.
@@ -278,7 +279,8 @@ LIME_API size_t lime_sequence_workspace_bytes(const lime_ctx* ctx, int32_t B, in
  * q_rows); out [q_rows x Hq x d_h], which overlaps no input.  A query that sees no key (more queries than keys, an empty history) gets zeros.  What a query does
  * not see has no influence on it, infinities and NaN included; what it sees has the influence that the formula gives: NaN where a score is
  * NaN or +infinity, or where all are -infinity.  bf16: products of bf16 values in fp32, probabilities rounded to bf16 for the value product
- * (their sum is not), one rounding of the result; fp32: all in fp32. */
+ * (their sum is not), one rounding of the result; fp32: all in fp32.  The weighted values are summed in fp32 before they are divided by
+ * the sum of the weights, each of up to 2^8: values beyond 2^119 divided by the number of keys that a row sees may become infinite. */
 LIME_API lime_status lime_attend_history(lime_ctx* ctx, const void* q, int64_t q_stride, const int32_t* off, const void* k,
                                 int64_t k_stride, const void* v, int64_t v_stride, const int32_t* kv_off, int32_t B, int64_t q_rows,
                                 int64_t kv_rows, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);

@@ -11,9 +11,10 @@
 // d_h <= 32 leaves columns for the probabilities, so that the next scores are formed while these are worked out.
 // What bounds it: the hand-overs between the warps, tile by tile.  With loads and contractions issued by one warp and three CTAs an SM,
 // candidate roots (32 users of 1000 behind 1024 rows, 8 heads of 32) took 189 us; without their exponentials and contractions still 178; with nothing
-// left but the hand-overs 130.  The exponentials alone would take about 70.  As it stands they take 172 and 100 ragged users of 0..1000
-// rows 65.  More CTAs an SM do not help: four with 80 registers a thread, the scores loaded twice, 180 and 63..67; three as above 189 and
-// 69; both slots of k_seq_attn_tc.cu in one CTA 172 and 72.
+// left but the hand-overs 130.  The exponentials alone would take about 70.  As it stands they take 161 and 100 ragged users of 0..1000
+// rows 62, with the special-function unit at 0.49 and 0.39 and the tensor pipe at 0.12 and 0.10.  More CTAs an SM do not help (beside 172 and
+// 65 with two): four with 80 registers a thread, the scores loaded twice, 180 and 63..67; three as above 189 and 69; both slots of
+// k_seq_attn_tc.cu in one CTA 172 and 72.
 // The rest is as in k_seq_attn_tc.cu: online softmax with lazy rescale, probabilities rounded to bf16 for the value product and summed
 // unrounded, features past d_h as zeros in shared memory only, value rows behind the end of a cached range zeroed there, items whose
 // result is not finite done again with what is not finite taken out of the tiles that mask anything.

@@ -13,7 +13,7 @@
 // The next keys are requested when the scores are formed, the next values when the products are.  A page has at least 16 rows, so 16
 // aligned keys lie in one; the lanes look up the pages of 32 steps at once.  Four warps share an item's keys and are joined in shared
 // memory; items are those of k_seq_schedule, dealt back and forth.
-// Measured: 64 events of 16 heads over 16..16384 rows of 4 heads of 128 (1.07 GB) 180 us, 5.99 TB/s, 0.92 of the copy rate (221 on
+// Measured: 64 events of 16 heads over 16..16384 rows of 4 heads of 128 (1.07 GB) 180 us, 5.98 TB/s, 0.91 of the copy rate (221 on
 // tcgen05); 256 over 512 rows of 4 heads of 32 24.5 us (53); 32 over 500..5000 rows of 8 heads of 64 44.6 us; one over 1000 rows of 2
 // heads of 64 11.6 us (17), nearly all of it the latency of three launches.
 // Online softmax, the reference raised when exceeded by 2^8; probabilities are rounded to bf16 for the value product (the operands of an

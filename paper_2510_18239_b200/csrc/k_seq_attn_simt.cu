@@ -9,9 +9,10 @@
 // copied (cp.async) while a tile is worked on.
 // A masked position is -1 among the probabilities of a tile that has one: its value row is then not touched at all, so that infinities
 // and NaN there stay there.
-// What bounds it: with many items FFMA and the shared-memory reads that feed it (64 histories of 512 rows, 8 heads of 64: 0.59 ms,
-// 29 TFLOP/s); with few the chain of a tile, about 5 us for a block that has an SM to itself, so two blocks share one where they fit (drafts
-// of 7 users 91 -> 74 us with pairs of products and predicates for what is masked).
+// What bounds it: with many items FFMA and the shared-memory reads that feed it (64 histories of 512 rows, 8 heads of 64: 0.60 ms,
+// 29 of 74 TFLOP/s); with few the chain of a tile, about 5 us for a block that has an SM to itself, so two blocks share one where they fit (drafts
+// of 7 users 91 -> 74 us with pairs of products and predicates for what is masked; the FMA pipe is then busy in 0.47 of the cycles, the
+// paths to shared memory in 0.51).
 #include <type_traits>
 
 #include "seq_common.cuh"

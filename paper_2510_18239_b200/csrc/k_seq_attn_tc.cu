@@ -22,13 +22,13 @@
 //  * Masked positions have p = 0, but 0 * NaN and 0 * infinity are NaN.  Value rows behind the end of a cached range, which may never have
 //    been written, are zeroed in shared memory.  Elsewhere such values are the exception: an item whose result has a NaN or an infinity is
 //    done again with what is not finite taken out of every tile that masks anything; the rows that do see it get it added at the end.
-// What bounds it: 16384 causal rows of 16 heads of 128 over 4 heads of keys take 1.08 to 1.12 ms, 0.98 to 1.02 PFLOP/s at 1.83 GHz and 950 to
-// 1000 W, the power cap: 2250 cycles of an SM for a tile of 128 x 128, of which its contractions fill 1024 of the tensor pipe and its
-// exponentials 1024 of the special-function unit.  A slot's chain (scores, maximum, exponentials, values) is longer than a tile's share of
-// either, and with two slots the one fills the gaps of the other only in part.  Measured and dropped: probabilities against the reference
-// of the tiles before, without waiting for the maximum (1.15 ms); 64-key tiles with two score buffers a slot, which take the scores out of
-// the chain (1.24 ms); two threads a row, 16 softmax warps (1.18 ms); the first half of the probabilities handed over early, polling
-// without a pause (no change).
+// What bounds it: 16384 causal rows of 16 heads of 128 over 4 heads of keys take 1.08 to 1.12 ms, 0.98 to 1.02 PFLOP/s at 950 to 1000 W, the
+// power cap: 1825 active cycles of an SM for a tile of 128 x 128 (counted in a call alone: 1.03 ms at 1.58 GHz), of which its contractions
+// fill 1024 of the tensor pipe (56 %) and its exponentials 1024 of the special-function unit (57 %).  A slot's chain (scores, maximum,
+// exponentials, values) is longer than a tile's share of either, and with two slots the one fills the gaps of the other only in part.
+// Measured and dropped: probabilities against the reference of the tiles before, without waiting for the maximum (1.15 ms); 64-key tiles
+// with two score buffers a slot, which take the scores out of the chain (1.24 ms); two threads a row, 16 softmax warps (1.18 ms); the first
+// half of the probabilities handed over early, polling without a pause (no change).
 // A few rows stream their keys at 0.70 of the copy rate (64 users' 4 drafts over 16..16384 rows, 1.07 GB: 234 us).
 #include "seq_tc.cuh"
 

@@ -1,4 +1,11 @@
 // What the tensor-core kernels of the sequence path's attention share (k_seq_attn_tc.cu, k_seq_attn_d64_tc.cu).
+//
+// Where a bounded wait gave up (lime_device_status): the barrier, by who waits.
+//   d_h > 64: loads 111 kv_empty, 123 q_empty; scores 112 q_full, 113 kv_full, 114 s_free; values 115 kv_full, 116 mend_done, 117 p_ready,
+//     124 o_free, 125 x_free; mending 118 kv_full, 119 mend_ask; softmax 120 s_full, 121 pv_done before a rescale, 122 pv_done at the end,
+//     126 ml_full, 127 ml_free; 110: shared memory not aligned
+//   d_h <= 64: loads 141 q_empty, 142 kv_empty; products 143 kv_full (keys), 144 q_full, 145 kv_full (values), 146 o_free, 147 p_ready, 151
+//     s_free; softmax 148 s_full, 149 pv_done of the tile before, 150 pv_done at the end; 140: shared memory not aligned
 #pragma once
 #include "seq_common.cuh"
 #include "tc_common.cuh"
