@@ -711,6 +711,8 @@ class Lime:
     # ---- the sequence path: attention over whole histories, with a cache of keys and values (for inference: no gradients are kept)
     def set_sequence(self, Hq: int, Hkv: int, d_h: int, attn_scale: float = 0.0, norm_eps: float = 0.0, rot_dim: int = 0,
                      rot_interleaved: bool = False, rot_base: float = 0.0) -> None:
+        """The shape that the calls below go by; 0 stands for the library's default.  They take no part in autograd: their results require
+        no gradient, whatever their inputs do."""
         lime_set_sequence(self.ctx, lime_sequence(Hq, Hkv, d_h, attn_scale, norm_eps, rot_dim, int(rot_interleaved), rot_base))
         self._seq = (self.tdtype == torch.bfloat16, Hq, Hkv, d_h)
 
